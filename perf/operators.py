@@ -1,0 +1,435 @@
+"""The operators of language models that stand beside the compiled expressions, as measurable cases.
+
+A training step around compiled expressions looks up tokens (embed), normalises rows (norm), keeps activations in 8 bits
+between forward and backward pass (pack) and multiplies 8-bit operands (product):
+
+  embed    y_t = s E[token_t]; its gradient dE_v = s sum over the t with token_t = v of dy_t, zeros where there is none
+  norm     y = (x - mean) rstd w + b over rows; dx, dw, db; the backward pass reads x or its 8-bit checkpoint
+  pack     blocks of 128 along a row in e4m3 with one power of two as scale: stored and loaded again, or turned (stored anew
+           with blocks along the other direction, as the gradient of a weight needs them)
+  product  y_mn = sum_k a_mk b_nk of packed operands
+
+Tokens follow the harmonic law of word frequencies; a small share of them is padding (-1): rows of zeros, no gradient.
+"""
+from __future__ import annotations
+
+import math
+
+import torch
+
+own = False
+
+BLOCK = 128
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+SIZE = {"f32": 4, "bf16": 2, "f16": 2}
+EPS = 1e-5
+
+
+def listed():
+    return [
+        # generation: one step of sixteen sequences looks up sixteen tokens
+        dict(name="embed_16_tokens", op="embed", way="forward", tokens=16, vocab=32000, width=4096, type="bf16", grad="f32"),
+        # a training step on 16384 tokens, odd vocabulary: lookup and the gradient in 32 bits
+        dict(name="embed_16384_step", op="embed", way="step", tokens=16384, vocab=50021, width=1024, type="bf16", grad="f32"),
+        # the gradient alone: large batch, large vocabulary
+        dict(name="embed_65536_gradient", op="embed", way="backward", tokens=65536, vocab=128000, width=2048, type="bf16", grad="f32"),
+        # generation: sixteen rows
+        dict(name="norm_16x4096", op="norm", way="forward", rows=16, width=4096, type="bf16", kept="x"),
+        # a training step
+        dict(name="norm_8192x4096_step", op="norm", way="step", rows=8192, width=4096, type="bf16", kept="x"),
+        # odd width: rows start off every boundary
+        dict(name="norm_5003x1001_step", op="norm", way="step", rows=5003, width=1001, type="f32", kept="x"),
+        # a training step that keeps its input in 8 bits
+        dict(name="norm_16384x2048_kept8", op="norm", way="step", rows=16384, width=2048, type="bf16", kept="packed"),
+        # an activation between forward and backward pass: stored, loaded again
+        dict(name="pack_16384x8192", op="pack", way="roundtrip", rows=16384, width=8192, type="bf16"),
+        # a kept activation as operand of a weight's gradient: blocks along the tokens, ragged sizes
+        dict(name="pack_5003x1537_turn", op="pack", way="turn", rows=5003, width=1537, type="f32"),
+        # one token through a layer
+        dict(name="product_1x4096x4096", op="product", m=1, n=4096, k=4096, type="bf16"),
+        # a layer of a training step
+        dict(name="product_8192x4096x4096", op="product", m=8192, n=4096, k=4096, type="bf16"),
+        # ragged sizes, a gradient kept in 32 bits
+        dict(name="product_1500x1333x1100", op="product", m=1500, n=1333, k=1100, type="f32"),
+    ]
+
+
+def _log_int(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def _within(rng, most, *ranges):
+    """sizes from log-uniform ranges whose product is at most `most`"""
+    while True:
+        v = [_log_int(rng, lo, hi) for lo, hi in ranges]
+        if math.prod(v) <= most:
+            return v
+
+
+def draw(rng):
+    op = rng.choice(["embed", "norm", "pack", "product"])
+    kind = rng.choice(["bf16", "bf16", "f32", "f16"])
+    if op == "embed":
+        while True:
+            t, v, w = _within(rng, 1 << 62, (1, 65536), (100, 128000), (16, 4096))
+            if t * w <= 65536 * 2048 and v * w <= 128000 * 2048:
+                break
+        if rng.random() < 0.5:
+            w = max(16, w // 8 * 8)
+        return dict(op=op, way=rng.choice(["forward", "backward", "step"]), tokens=t, vocab=v, width=w, type=kind,
+                    grad=rng.choice(["f32", "f32", "bf16"]))
+    if op == "product":
+        m, n, k = _within(rng, 8192 * 4096 * 4096, (1, 8192), (16, 8192), (16, 8192))
+        return dict(op=op, m=m, n=n, k=k, type=kind)
+    r, w = _within(rng, 8192 * 4096, (1, 32768), (8, 16384))
+    if rng.random() < 0.5:
+        w = max(8, w // 8 * 8)
+    if op == "norm":
+        return dict(op=op, way=rng.choice(["forward", "backward", "step", "step"]), rows=r, width=w, type=kind,
+                    kept=rng.choice(["x", "x", "packed"]))
+    return dict(op=op, way=rng.choice(["roundtrip", "turn"]), rows=r, width=w, type=kind)
+
+
+# ---- 8-bit blocks, in plain operations ----
+
+def _blocks(n):
+    return -(-n // BLOCK)
+
+
+def _padded(n):
+    return -(-n // 16) * 16
+
+
+def _scales(x):
+    """the power of two of every block of 128 of a row: the least 2^k, k >= -126, with amax <= 448 2^k; 1 for zeros"""
+    r, w = x.shape
+    a = torch.where(torch.isfinite(x), x.abs(), torch.zeros_like(x))
+    a = torch.nn.functional.pad(a, (0, _blocks(w) * BLOCK - w)).view(r, _blocks(w), BLOCK).amax(2)
+    m, e = torch.frexp(a)                       # a = m 2^e, m in [0.5, 1); 448 = 0.875 2^9
+    k = torch.where(m > 0.875, e - 8, e - 9).clamp(min=-126)
+    return torch.where(a > 0, torch.ldexp(torch.ones_like(a), k), torch.ones_like(a))
+
+
+def _spread(s, w):
+    return s.repeat_interleave(BLOCK, dim=1)[:, :w]
+
+
+def _pack(x):
+    """(e4m3 values, scales) of a 32-bit matrix"""
+    s = _scales(x)
+    return (x / _spread(s, x.shape[1])).to(torch.float8_e4m3fn), s
+
+
+def _unpack(q, s):
+    return q.float() * _spread(s, q.shape[1])
+
+
+def _store(x):
+    """a packed matrix as a program keeps it: bytes with rows of a multiple of 16, and scales"""
+    r, w = x.shape
+    q, s = _pack(x)
+    b = torch.zeros((r, _padded(w)), dtype=torch.uint8, device=x.device)
+    b[:, :w] = q.view(torch.uint8)
+    return b, s.contiguous()
+
+
+def _room(r, w):
+    return (torch.zeros((r, _padded(w)), dtype=torch.uint8, device="cuda"),
+            torch.ones((r, _blocks(w)), dtype=torch.float32, device="cuda"))
+
+
+def _values(b, w):
+    return b.view(torch.float8_e4m3fn)[:, :w]
+
+
+# ---- inputs ----
+
+def prepare(case, seed):
+    dev = torch.device("cuda")
+    g = torch.Generator(device=dev)
+    g.manual_seed(int(seed))
+    c, op = case, case["op"]
+    kind = TYPES[c["type"]]
+
+    def normal(*shape, scale=1.0, shift=0.0, to=kind):
+        return (torch.randn(shape, generator=g, device=dev) * scale + shift).to(to)
+
+    s = dict(case=c)
+    if op == "embed":
+        t, v, w = c["tokens"], c["vocab"], c["width"]
+        u = torch.rand(t, generator=g, device=dev, dtype=torch.float64)
+        tok = (torch.exp(u * math.log(v + 1.0)) - 1.0).long().clamp(0, v - 1)
+        pad = torch.rand(t, generator=g, device=dev) < 0.02
+        s["tokens"] = torch.where(pad, torch.full_like(tok, -1), tok).int()
+        s["scale"] = math.sqrt(w)
+        if c["way"] != "backward":
+            s["table"] = normal(v, w, scale=0.02)
+            s["y"] = torch.empty((t, w), dtype=kind, device=dev)
+        if c["way"] != "forward":
+            s["dy"] = normal(t, w)
+            s["dtable"] = torch.empty((v, w), dtype=TYPES[c["grad"]], device=dev)
+        return s
+    if op == "norm":
+        r, w = c["rows"], c["width"]
+        # a residual stream: rows of different size and a mean that is a part of their spread
+        size = torch.exp(0.5 * torch.randn((r, 1), generator=g, device=dev))
+        x = torch.randn((r, w), generator=g, device=dev) * size + 0.2 * torch.randn((r, 1), generator=g, device=dev)
+        s["x"] = x.to(kind)
+        s["w"] = normal(w, scale=0.1, shift=1.0)
+        s["b"] = normal(w, scale=0.1)
+        s["y"] = torch.empty((r, w), dtype=kind, device=dev)
+        s["mean"], s["rstd"] = (torch.empty(r, device=dev) for _ in range(2))
+        if c["kept"] == "packed":
+            s["q"], s["s"] = _room(r, w)
+        if c["way"] == "backward":
+            x = s["x"].float()
+            s["mean"] = x.mean(1)
+            s["rstd"] = torch.rsqrt((x - s["mean"][:, None]).square().mean(1) + EPS)
+            if c["kept"] == "packed":
+                s["q"], s["s"] = _store(x)
+        if c["way"] != "forward":
+            s["dy"] = normal(r, w)
+            s["dx"] = torch.empty((r, w), dtype=kind, device=dev)
+            s["dw"], s["db"] = (torch.empty(w, device=dev) for _ in range(2))
+        return s
+    if op == "pack":
+        r, w = c["rows"], c["width"]
+        x = normal(r, w, to=torch.float32) * torch.exp(torch.randn((r, 1), generator=g, device=dev))
+        if c["way"] == "roundtrip":
+            s["x"] = x.to(kind)
+            s["q"], s["s"] = _room(r, w)
+            s["back"] = torch.empty((r, w), dtype=kind, device=dev)
+        else:
+            s["q"], s["s"] = _store(x)
+            s["tq"], s["ts"] = _room(w, r)
+        return s
+    s["a"], s["sa"] = _store(normal(c["m"], c["k"], to=torch.float32))
+    s["b"], s["sb"] = _store(normal(c["n"], c["k"], scale=1.0 / math.sqrt(c["k"]), to=torch.float32))
+    s["y"] = torch.empty((c["m"], c["n"]), dtype=kind, device=dev)
+    return s
+
+
+# ---- one pass ----
+
+def run(state):
+    if own:
+        return _run_own(state)
+    return {"embed": _embed, "norm": _norm, "pack": _pack_pass, "product": _product}[state["case"]["op"]](state)
+
+
+def _embed(s):
+    c, out = s["case"], {}
+    tok = s["tokens"].long()
+    live = (tok >= 0) & (tok < c["vocab"])
+    if c["way"] != "backward":
+        y = s["table"][tok.clamp(0, c["vocab"] - 1)].float() * s["scale"]
+        out["y"] = torch.where(live[:, None], y, torch.zeros_like(y)).to(TYPES[c["type"]])
+    if c["way"] != "forward":
+        d = torch.zeros((c["vocab"] + 1, c["width"]), device=tok.device)
+        d.index_add_(0, torch.where(live, tok, torch.full_like(tok, c["vocab"])), s["dy"].float())
+        out["dtable"] = (d[:-1] * s["scale"]).to(TYPES[c["grad"]])
+    return out
+
+
+def _norm(s):
+    c, out = s["case"], {}
+    kind, w = TYPES[c["type"]], s["w"].float()
+    mean, rstd = s["mean"], s["rstd"]
+    if c["way"] != "backward":
+        x = s["x"].float()
+        mean = x.mean(1)
+        rstd = torch.rsqrt((x - mean[:, None]).square().mean(1) + EPS)
+        y = ((x - mean[:, None]) * rstd[:, None]) * w + s["b"].float()
+        out = dict(y=y.to(kind), mean=mean, rstd=rstd)
+        if c["kept"] == "packed":
+            out["kept"], out["scales"] = _pack(x)
+    if c["way"] != "forward":
+        if c["kept"] == "packed":
+            x = _unpack(out["kept"], out["scales"]) if "kept" in out else _unpack(_values(s["q"], c["width"]), s["s"])
+        else:
+            x = s["x"].float()
+        dy = s["dy"].float()
+        xh = (x - mean[:, None]) * rstd[:, None]
+        g = dy * w
+        dx = (g - g.mean(1, keepdim=True) - xh * (g * xh).mean(1, keepdim=True)) * rstd[:, None]
+        out["dx"], out["dw"], out["db"] = dx.to(kind), (dy * xh).sum(0), dy.sum(0)
+    return out
+
+
+def _pack_pass(s):
+    c = s["case"]
+    if c["way"] == "roundtrip":
+        q, sc = _pack(s["x"].float())
+        return dict(q=q, scales=sc, back=_unpack(q, sc).to(TYPES[c["type"]]))
+    q, sc = _pack(_unpack(_values(s["q"], c["width"]), s["s"]).t().contiguous())
+    return dict(q=q, scales=sc)
+
+
+def _product(s):
+    c = s["case"]
+    a = _unpack(_values(s["a"], c["k"]), s["sa"])
+    b = _unpack(_values(s["b"], c["k"]), s["sb"])
+    return dict(y=(a @ b.t()).to(TYPES[c["type"]]))
+
+
+def _workspace(s, n):
+    """room that the program keeps between calls"""
+    if s.get("ws") is None or s["ws"].numel() < n:
+        s["ws"] = torch.empty(max(256, n), dtype=torch.uint8, device="cuda")
+    return dict(workspace_ptr=s["ws"].data_ptr(), workspace_bytes=s["ws"].numel())
+
+
+def _run_own(s):
+    import paper_1711_01348_b200 as tad
+
+    def rows(t):
+        name = {torch.float32: "f32", torch.bfloat16: "bf16", torch.float16: "f16"}[t.dtype]
+        return tad.Rows(t.data_ptr(), t.stride(0), name)
+
+    def packed(q, sc):
+        return tad.Packed(q.data_ptr(), sc.data_ptr(), q.stride(0), sc.stride(0))
+
+    c, op, out = s["case"], s["case"]["op"], {}
+    stream = torch.cuda.current_stream().cuda_stream
+    if op == "embed":
+        t, v, w = c["tokens"], c["vocab"], c["width"]
+        if c["way"] != "backward":
+            tad.embed_forward(s["tokens"].data_ptr(), 32, t, rows(s["table"]), v, w, s["scale"], rows(s["y"]), stream=stream)
+            out["y"] = s["y"]
+        if c["way"] != "forward":
+            tad.embed_backward(s["tokens"].data_ptr(), 32, t, rows(s["dy"]), v, w, s["scale"], rows(s["dtable"]), stream=stream,
+                               **_workspace(s, tad.embed_workspace_bytes(t, v, w)))
+            out["dtable"] = s["dtable"]
+        return out
+    if op == "norm":
+        r, w = c["rows"], c["width"]
+        kept = packed(s["q"], s["s"]) if c["kept"] == "packed" else None
+        if c["way"] != "backward":
+            tad.layernorm_forward(rows(s["x"]), r, w, rows(s["y"]), weight=rows(s["w"]), bias=rows(s["b"]), eps=EPS,
+                                  mean_ptr=s["mean"].data_ptr(), rstd_ptr=s["rstd"].data_ptr(), checkpoint=kept, stream=stream)
+            out = dict(y=s["y"], mean=s["mean"], rstd=s["rstd"])
+            if kept:
+                out["kept"], out["scales"] = _values(s["q"], w), s["s"]
+        if c["way"] != "forward":
+            tad.layernorm_backward(rows(s["dy"]), None if kept else rows(s["x"]), kept, r, w, s["mean"].data_ptr(),
+                                   s["rstd"].data_ptr(), rows(s["dx"]), weight=rows(s["w"]), dweight=rows(s["dw"]),
+                                   dbias=rows(s["db"]), stream=stream, **_workspace(s, tad.layernorm_workspace_bytes(r, w)))
+            out.update(dx=s["dx"], dw=s["dw"], db=s["db"])
+        return out
+    if op == "pack":
+        r, w = c["rows"], c["width"]
+        if c["way"] == "roundtrip":
+            tad.pack8(rows(s["x"]), r, w, packed(s["q"], s["s"]), stream=stream)
+            tad.unpack8(packed(s["q"], s["s"]), r, w, rows(s["back"]), stream=stream)
+            return dict(q=_values(s["q"], w), scales=s["s"], back=s["back"])
+        tad.repack8(packed(s["q"], s["s"]), r, w, packed(s["tq"], s["ts"]), stream=stream)
+        return dict(q=_values(s["tq"], r), scales=s["ts"])
+    tad.matmul8(packed(s["a"], s["sa"]), packed(s["b"], s["sb"]), c["m"], c["n"], c["k"], rows(s["y"]), stream=stream,
+                **_workspace(s, tad.matmul8_workspace_bytes(c["m"], c["n"], c["k"])))
+    return dict(y=s["y"])
+
+
+# ---- what a pass cannot do without ----
+
+def work(case):
+    c, op = case, case["op"]
+    e = SIZE[c["type"]]
+    if op == "embed":
+        t, v, w = c["tokens"], c["vocab"], c["width"]
+        n = f = 0.0
+        if c["way"] != "backward":
+            n += 4.0 * t + (min(t, v) + t) * w * e
+            f += t * w
+        if c["way"] != "forward":
+            n += 4.0 * t + t * w * e + v * w * SIZE[c["grad"]]
+            f += t * w
+        return {"bytes": n, "flops": f}
+    if op == "product":
+        m, n, k = c["m"], c["n"], c["k"]
+        return {"bytes": (m + n) * (k + 4.0 * _blocks(k)) + m * n * e, "flops": 2.0 * m * n * k}
+    r, w = c["rows"], c["width"]
+    x8 = r * (w + 4.0 * _blocks(w))
+    if op == "pack":
+        if c["way"] == "roundtrip":
+            return {"bytes": 2.0 * r * w * e + 2 * x8, "flops": 3.0 * r * w}
+        return {"bytes": x8 + w * (r + 4.0 * _blocks(r)), "flops": 3.0 * r * w}
+    n = f = 0.0
+    if c["way"] != "backward":
+        n += 2.0 * r * w * e + 8.0 * r + 2 * w * e + (x8 if c["kept"] == "packed" else 0.0)
+        f += 8.0 * r * w
+    if c["way"] != "forward":
+        n += 2.0 * r * w * e + (x8 if c["kept"] == "packed" else r * w * e) + 8.0 * r + w * e + 8.0 * w
+        f += 14.0 * r * w
+    return {"bytes": n, "flops": f}
+
+
+# ---- the definitions in 64 bits ----
+
+def _e4m3_near(v):
+    """the e4m3 value nearest to every |v| <= 448 (ties to the even significand), from the definition of the format"""
+    exponent = torch.floor(torch.log2(v.abs().clamp(min=2.0 ** -40))).clamp(min=-6.0)
+    step = torch.exp2(exponent - 3.0)           # three bits behind the leading one; subnormal numbers step 2^-9
+    return torch.round(v / step) * step         # (a value that rounds up to the next power of two is that power)
+
+
+def _kept(x):
+    """(values, scales, values times scales) of the 8-bit blocks of a 64-bit matrix"""
+    r, w = x.shape
+    nb = _blocks(w)
+    p = torch.zeros((r, nb * BLOCK), dtype=torch.float64, device=x.device)
+    p[:, :w] = x
+    p = p.view(r, nb, BLOCK)
+    a = p.abs().amax(2)
+    k = torch.ceil(torch.log2(a.clamp(min=1e-300) / 448.0))
+    k = torch.where(a > 448.0 * torch.exp2(k), k + 1, k)              # (a logarithm may be off by its last bit)
+    k = torch.where(a <= 448.0 * torch.exp2(k - 1), k - 1, k).clamp(min=-126.0)
+    s = torch.where(a > 0, torch.exp2(k), torch.ones_like(a))
+    q = _e4m3_near(p / s[:, :, None])
+    return q.view(r, -1)[:, :w], s, (q * s[:, :, None]).view(r, -1)[:, :w]
+
+
+def _stood_for(b, s, w):
+    v = b.view(torch.float8_e4m3fn).double()
+    return (v * torch.nn.functional.pad(s.double().repeat_interleave(BLOCK, 1), (0, 16))[:, :v.shape[1]])[:, :w]
+
+
+def exact(case, seed):
+    s, c, op = prepare(case, seed), case, case["op"]
+    if op == "embed":
+        t, v, w = c["tokens"], c["vocab"], c["width"]
+        tok, out = s["tokens"].long(), {}
+        at = torch.nonzero((tok >= 0) & (tok < v)).flatten()
+        if c["way"] != "backward":
+            out["y"] = torch.zeros((t, w), dtype=torch.float64, device=tok.device)
+            out["y"][at] = s["table"].double()[tok[at]] * s["scale"]
+        if c["way"] != "forward":
+            out["dtable"] = torch.zeros((v, w), dtype=torch.float64, device=tok.device)
+            out["dtable"].index_put_((tok[at],), s["dy"].double()[at] * s["scale"], accumulate=True)
+        return out
+    if op == "product":
+        return dict(y=_stood_for(s["a"], s["sa"], c["k"]) @ _stood_for(s["b"], s["sb"], c["k"]).t())
+    if op == "pack":
+        if c["way"] == "roundtrip":
+            q, sc, back = _kept(s["x"].double())
+            return dict(q=q, scales=sc, back=back)
+        q, sc, _ = _kept(_stood_for(s["q"], s["s"], c["width"]).t())
+        return dict(q=q, scales=sc)
+    x, w, out = s["x"].double(), s["w"].double(), {}
+    if c["way"] == "backward":
+        mean, rstd = s["mean"].double(), s["rstd"].double()
+    else:
+        mean = x.sum(1) / c["width"]
+        rstd = 1.0 / torch.sqrt(((x - mean[:, None]) ** 2).sum(1) / c["width"] + EPS)
+        out = dict(y=(x - mean[:, None]) * rstd[:, None] * w + s["b"].double(), mean=mean, rstd=rstd)
+    if c["kept"] == "packed":
+        q, sc, back = _kept(x)
+        if c["way"] != "backward":
+            out.update(kept=q, scales=sc)
+        x = back
+    if c["way"] != "forward":
+        dy = s["dy"].double()
+        xh = (x - mean[:, None]) * rstd[:, None]
+        g = dy * w
+        a, b = g.sum(1) / c["width"], (g * xh).sum(1) / c["width"]
+        out.update(dx=rstd[:, None] * (g - a[:, None] - b[:, None] * xh), dw=torch.einsum("rw,rw->w", dy, xh), db=dy.sum(0))
+    return out
