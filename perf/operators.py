@@ -96,11 +96,7 @@ def _blocks(n):
     return -(-n // BLOCK)
 
 
-def _padded(n):
-    return -(-n // 16) * 16
-
-
-def _scales(x):
+def _powers(x):
     """the power of two of every block of 128 of a row: the least 2^k, k >= -126, with amax <= 448 2^k; 1 for zeros"""
     r, w = x.shape
     a = torch.where(torch.isfinite(x), x.abs(), torch.zeros_like(x))
@@ -115,31 +111,36 @@ def _spread(s, w):
 
 
 def _pack(x):
-    """(e4m3 values, scales) of a 32-bit matrix"""
-    s = _scales(x)
-    return (x / _spread(s, x.shape[1])).to(torch.float8_e4m3fn), s
+    """(e4m3 values, scales) of a 32-bit matrix; a scale is held as its exponent"""
+    s = _powers(x)
+    return (x / _spread(s, x.shape[1])).to(torch.float8_e4m3fn), s.to(torch.float8_e8m0fnu)
 
 
 def _unpack(q, s):
-    return q.float() * _spread(s, q.shape[1])
-
-
-def _store(x):
-    """a packed matrix as a program keeps it: bytes with rows of a multiple of 16, and scales"""
-    r, w = x.shape
-    q, s = _pack(x)
-    b = torch.zeros((r, _padded(w)), dtype=torch.uint8, device=x.device)
-    b[:, :w] = q.view(torch.uint8)
-    return b, s.contiguous()
+    return q.float() * _spread(s.float(), q.shape[1])
 
 
 def _room(r, w):
-    return (torch.zeros((r, _padded(w)), dtype=torch.uint8, device="cuda"),
-            torch.ones((r, _blocks(w)), dtype=torch.float32, device="cuda"))
+    """a packed matrix as a program keeps it: rows of a multiple of 16 bytes, scales in rows of a multiple of 4"""
+    return (torch.zeros((r, -(-w // 16) * 16), dtype=torch.uint8, device="cuda"),
+            torch.full((r, -(-_blocks(w) // 4) * 4), 127, dtype=torch.uint8, device="cuda"))
+
+
+def _store(x):
+    r, w = x.shape
+    q, s = _pack(x)
+    b, e = _room(r, w)
+    b[:, :w] = q.view(torch.uint8)
+    e[:, :_blocks(w)] = s.view(torch.uint8)
+    return b, e
 
 
 def _values(b, w):
     return b.view(torch.float8_e4m3fn)[:, :w]
+
+
+def _scales(e, w):
+    return e.view(torch.float8_e8m0fnu)[:, :_blocks(w)]
 
 
 # ---- inputs ----
@@ -245,7 +246,7 @@ def _norm(s):
             out["kept"], out["scales"] = _pack(x)
     if c["way"] != "forward":
         if c["kept"] == "packed":
-            x = _unpack(out["kept"], out["scales"]) if "kept" in out else _unpack(_values(s["q"], c["width"]), s["s"])
+            x = _unpack(out["kept"], out["scales"]) if "kept" in out else _unpack(_values(s["q"], c["width"]), _scales(s["s"], c["width"]))
         else:
             x = s["x"].float()
         dy = s["dy"].float()
@@ -261,14 +262,14 @@ def _pack_pass(s):
     if c["way"] == "roundtrip":
         q, sc = _pack(s["x"].float())
         return dict(q=q, scales=sc, back=_unpack(q, sc).to(TYPES[c["type"]]))
-    q, sc = _pack(_unpack(_values(s["q"], c["width"]), s["s"]).t().contiguous())
+    q, sc = _pack(_unpack(_values(s["q"], c["width"]), _scales(s["s"], c["width"])).t().contiguous())
     return dict(q=q, scales=sc)
 
 
 def _product(s):
     c = s["case"]
-    a = _unpack(_values(s["a"], c["k"]), s["sa"])
-    b = _unpack(_values(s["b"], c["k"]), s["sb"])
+    a = _unpack(_values(s["a"], c["k"]), _scales(s["sa"], c["k"]))
+    b = _unpack(_values(s["b"], c["k"]), _scales(s["sb"], c["k"]))
     return dict(y=(a @ b.t()).to(TYPES[c["type"]]))
 
 
@@ -309,7 +310,7 @@ def _run_own(s):
                                   mean_ptr=s["mean"].data_ptr(), rstd_ptr=s["rstd"].data_ptr(), checkpoint=kept, stream=stream)
             out = dict(y=s["y"], mean=s["mean"], rstd=s["rstd"])
             if kept:
-                out["kept"], out["scales"] = _values(s["q"], w), s["s"]
+                out["kept"], out["scales"] = _values(s["q"], w), _scales(s["s"], w)
         if c["way"] != "forward":
             tad.layernorm_backward(rows(s["dy"]), None if kept else rows(s["x"]), kept, r, w, s["mean"].data_ptr(),
                                    s["rstd"].data_ptr(), rows(s["dx"]), weight=rows(s["w"]), dweight=rows(s["dw"]),
@@ -321,9 +322,9 @@ def _run_own(s):
         if c["way"] == "roundtrip":
             tad.pack8(rows(s["x"]), r, w, packed(s["q"], s["s"]), stream=stream)
             tad.unpack8(packed(s["q"], s["s"]), r, w, rows(s["back"]), stream=stream)
-            return dict(q=_values(s["q"], w), scales=s["s"], back=s["back"])
+            return dict(q=_values(s["q"], w), scales=_scales(s["s"], w), back=s["back"])
         tad.repack8(packed(s["q"], s["s"]), r, w, packed(s["tq"], s["ts"]), stream=stream)
-        return dict(q=_values(s["tq"], r), scales=s["ts"])
+        return dict(q=_values(s["tq"], r), scales=_scales(s["ts"], r))
     tad.matmul8(packed(s["a"], s["sa"]), packed(s["b"], s["sb"]), c["m"], c["n"], c["k"], rows(s["y"]), stream=stream,
                 **_workspace(s, tad.matmul8_workspace_bytes(c["m"], c["n"], c["k"])))
     return dict(y=s["y"])
@@ -346,13 +347,13 @@ def work(case):
         return {"bytes": n, "flops": f}
     if op == "product":
         m, n, k = c["m"], c["n"], c["k"]
-        return {"bytes": (m + n) * (k + 4.0 * _blocks(k)) + m * n * e, "flops": 2.0 * m * n * k}
+        return {"bytes": (m + n) * (k + 1.0 * _blocks(k)) + m * n * e, "flops": 2.0 * m * n * k}
     r, w = c["rows"], c["width"]
-    x8 = r * (w + 4.0 * _blocks(w))
+    x8 = r * (w + 1.0 * _blocks(w))
     if op == "pack":
         if c["way"] == "roundtrip":
             return {"bytes": 2.0 * r * w * e + 2 * x8, "flops": 3.0 * r * w}
-        return {"bytes": x8 + w * (r + 4.0 * _blocks(r)), "flops": 3.0 * r * w}
+        return {"bytes": x8 + w * (r + 1.0 * _blocks(r)), "flops": 3.0 * r * w}
     n = f = 0.0
     if c["way"] != "backward":
         n += 2.0 * r * w * e + 8.0 * r + 2 * w * e + (x8 if c["kept"] == "packed" else 0.0)
@@ -388,9 +389,10 @@ def _kept(x):
     return q.view(r, -1)[:, :w], s, (q * s[:, :, None]).view(r, -1)[:, :w]
 
 
-def _stood_for(b, s, w):
-    v = b.view(torch.float8_e4m3fn).double()
-    return (v * torch.nn.functional.pad(s.double().repeat_interleave(BLOCK, 1), (0, 16))[:, :v.shape[1]])[:, :w]
+def _stood_for(b, e, w):
+    v = b.view(torch.float8_e4m3fn)[:, :w].double()
+    k = torch.arange(w, device=b.device) // BLOCK
+    return v * torch.exp2(e[:, k].double() - 127.0)
 
 
 def exact(case, seed):
