@@ -271,6 +271,114 @@ tad_status tad_measure_fp32_rate(void *cuda_stream, double *tflops);
 tad_status tad_debug_status(const tad_plan *plan, void *workspace, void *cuda_stream);
 
 /* ------------------------------------------------------------------------- */
+/* Operators of language models beside the compiled expressions: lookups by    */
+/* tokens, norms of rows, activations in 8 bits and products of them.          */
+/* ------------------------------------------------------------------------- */
+
+/*
+ * What a training step needs around compiled expressions and what no expression says: an index that is data, statistics of
+ * a row, 16-bit tensors, 8-bit operands.  The gradients follow the rule of tad_backward: gather form, one owner per element,
+ * no floating-point atomics, sums in a fixed order and in fp32 (two calls on the same data give the same bits).
+ *   - Pointers are DEVICE pointers of the current device; work is enqueued on the given stream, nothing is allocated and
+ *     nothing synchronises; every call may be captured into a graph.  Descriptors (tad_rows, tad_packed) are host
+ *     structures, read before the call returns.  Outputs must not overlap inputs or each other.
+ *   - A matrix that is written is written in its n_rows x width elements only: what lies between its rows and behind
+ *     them keeps its bytes.
+ *   - Workspaces: device memory of at least the bytes that the matching function says, 256-byte aligned, owned by the
+ *     caller; its content need not be kept between calls, and calls that share one must not overlap on the device.
+ *   - Limits: 0 <= n_rows, n_tokens < 2^31, 0 <= width < 2^24; offsets are computed in 64 bits.  Sizes of zero are
+ *     allowed; TAD_ERR_UNSUPPORTED beyond.  NULL descriptors or data that a call needs, a stride below the width, an unknown
+ *     type, a misaligned packed matrix: TAD_ERR_INVALID_ARG.
+ */
+typedef enum { TAD_F32 = 0, TAD_BF16 = 1, TAD_F16 = 2 } tad_type;
+
+/* A matrix: rows of contiguous elements of one type, `stride` elements from one row to the next (any, at least the width).
+ * data needs the alignment of its element only; 16-byte aligned rows are faster.  A vector is a matrix of one row (its
+ * stride is not looked at). */
+typedef struct {
+    void *data;
+    int64_t stride;
+    int32_t type;            /* tad_type */
+    int32_t reserved;        /* must be zero */
+} tad_rows;
+
+/* A matrix in 8 bits: element (r, c) is  e4m3(q[r q_stride + c]) * 2^(scale[r scale_stride + c / 128] - 127).
+ * q is 16-byte aligned and q_stride a multiple of 16 (bytes), at least the width; scale is 4-byte aligned and scale_stride a
+ * multiple of 4, at least the number of blocks of 128 in a row; the last row has the length of the others.  e4m3: sign,
+ * four bits of exponent, three of fraction, largest value 448, no infinity, 0x7f / 0xff NaN. */
+#define TAD_BLOCK8 128
+typedef struct {
+    uint8_t *q;
+    uint8_t *scale;
+    int64_t q_stride;
+    int64_t scale_stride;
+} tad_packed;
+
+/*
+ * tad_pack8: a matrix into 8 bits, an activation that is kept for the backward pass or an operand of tad_matmul8.  Each block of
+ * 128 elements of a row (the last one may be shorter) has the scale 2^k, k the least integer >= -126 with
+ * max |x| <= 448 2^k over its finite elements (k = 0 where all are zero); q = e4m3(x / 2^k), rounded to nearest, ties to even.
+ * The division is exact, so an element is off by at most 2^-4 of its value or 2^(k-10), and the result is the same on every
+ * run.  Infinities and NaNs become NaN.
+ * tad_unpack8 gives q 2^k back, rounded to the type of x: exactly in fp32, and in bf16 for k >= -124 (but the largest numbers
+ * of either, which pack8 may have rounded up to 2^128, come back as infinities).
+ * tad_repack8 packs the transpose of a packed matrix: in is n_rows x width, out width x n_rows with blocks of 128 along
+ * what were the rows of `in` - the form in which a product that sums over the rows (the gradient of a weight) reads it.
+ * NaNs stay; the values of `in` are taken as they are (q 2^k in fp32) and rounded once more.
+ */
+tad_status tad_pack8(const tad_rows *x, int64_t n_rows, int64_t width, const tad_packed *out, void *cuda_stream);
+tad_status tad_unpack8(const tad_packed *in, int64_t n_rows, int64_t width, const tad_rows *x, void *cuda_stream);
+tad_status tad_repack8(const tad_packed *in, int64_t n_rows, int64_t width, const tad_packed *out, void *cuda_stream);
+
+/*
+ * tad_layernorm_forward:  y = (x - mean) rstd weight + bias  over each row, mean = sum x / width,
+ * rstd = 1 / sqrt(sum (x - mean)^2 / width + eps), statistics in fp32.
+ *   weight, bias   vectors of `width` elements; NULL = ones, zeros
+ *   mean, rstd     n_rows floats each, what the backward pass needs; NULL = not wanted
+ *   checkpoint     NULL, or x in 8 bits exactly as tad_pack8 gives it, written in the same pass
+ * y may have another type than x.
+ * tad_layernorm_backward:  with xh = (x - mean) rstd and g = dy weight,
+ *     dx = rstd (g - mean(g) - xh mean(g xh)),   dweight = sum over rows of dy xh,   dbias = sum over rows of dy.
+ *   x, checkpoint  the input of the forward pass, or what it kept in 8 bits: exactly one of the two.  From a checkpoint the
+ *                  gradients are those of the formula at the kept values, with the mean and rstd of the exact ones.
+ *   dx, dweight, dbias   NULL = not wanted.  dx may have another type than x.  Without rows dweight and dbias are zeros.
+ * Workspace: tad_layernorm_workspace_bytes, needed where dweight or dbias is wanted.
+ */
+tad_status tad_layernorm_forward(const tad_rows *x, int64_t n_rows, int64_t width, const tad_rows *weight, const tad_rows *bias,
+                                 float eps, const tad_rows *y, float *mean, float *rstd, const tad_packed *checkpoint,
+                                 void *cuda_stream);
+size_t tad_layernorm_workspace_bytes(int64_t n_rows, int64_t width);
+tad_status tad_layernorm_backward(const tad_rows *dy, const tad_rows *x, const tad_packed *checkpoint, int64_t n_rows, int64_t width,
+                                  const tad_rows *weight, const float *mean, const float *rstd, const tad_rows *dx,
+                                  const tad_rows *dweight, const tad_rows *dbias, void *workspace, size_t workspace_bytes,
+                                  void *cuda_stream);
+
+/*
+ * tad_embed_forward:  y[t] = factor * table[tokens[t]], a row of zeros where the token lies outside [0, n_table) (padding).
+ * tad_embed_backward: dtable[v] = factor * sum over the t with tokens[t] = v of dy[t], zeros where there is none; with
+ * accumulate != 0 the sum is added to what dtable holds and rows without a token are left alone.  Tokens outside the table
+ * give nothing.  The positions are sorted by token (stable), so every row is summed by its owners in ascending t.
+ *   tokens, token_bits   n_tokens integers of 32 or 64 bits
+ */
+tad_status tad_embed_forward(const void *tokens, int32_t token_bits, int64_t n_tokens, const tad_rows *table, int64_t n_table,
+                             int64_t width, float factor, const tad_rows *y, void *cuda_stream);
+size_t tad_embed_workspace_bytes(int64_t n_tokens, int64_t n_table, int64_t width);
+tad_status tad_embed_backward(const void *tokens, int32_t token_bits, int64_t n_tokens, const tad_rows *dy, int64_t n_table,
+                              int64_t width, float factor, const tad_rows *dtable, int32_t accumulate, void *workspace,
+                              size_t workspace_bytes, void *cuda_stream);
+
+/*
+ * tad_matmul8:  y[i, j] = sum over k of a[i, k] b[j, k],  a m x k and b n x k packed, y m x n.  Products of the 8-bit values and
+ * the scales are exact, sums are kept in fp32 (the tensor cores truncate where they align summands), y is rounded once.
+ * Forward, and both gradients, of a linear layer y = x w^T:  (x, w);  dx = (dy, w^T);  dw = (dy^T, x^T), the transposes by
+ * tad_repack8.  NaN operands give NaN in the row or column they belong to.  m, n < 2^31, k < 2^24.
+ * Workspace: tad_matmul8_workspace_bytes (may be 0); planes of partial sums of products with few outputs.
+ */
+size_t tad_matmul8_workspace_bytes(int64_t m, int64_t n, int64_t k);
+tad_status tad_matmul8(const tad_packed *a, const tad_packed *b, int64_t m, int64_t n, int64_t k, const tad_rows *y,
+                       void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/* ------------------------------------------------------------------------- */
 /* Introspection (host only).  These are what the bit-exact plan tests use.   */
 /* ------------------------------------------------------------------------- */
 

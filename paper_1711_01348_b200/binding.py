@@ -27,7 +27,10 @@ EXPORTS = ["tad_compile", "tad_destroy", "tad_workspace_bytes", "tad_forward", "
            "tad_staging_bytes", "tad_step_host", "tad_last_error", "tad_debug_status",
            "tad_plan_access_info", "tad_plan_bound_row", "tad_plan_enumerate", "tad_plan_kernel_stats",
            "tad_plan_disassemble", "tad_plan_print", "tad_extended_euclid", "tad_smith_normal_form", "tad_fourier_motzkin",
-           "tad_measure_fp32_rate"]
+           "tad_measure_fp32_rate",
+           "tad_pack8", "tad_unpack8", "tad_repack8", "tad_layernorm_forward", "tad_layernorm_workspace_bytes",
+           "tad_layernorm_backward", "tad_embed_forward", "tad_embed_workspace_bytes", "tad_embed_backward",
+           "tad_matmul8_workspace_bytes", "tad_matmul8"]
 
 
 class TadError(RuntimeError):
@@ -76,6 +79,25 @@ class KernelStats(C.Structure):
                 ("bytecode_words", C.c_int32), ("n_launches", C.c_int32)]
 
 
+TYPE = {"f32": 0, "bf16": 1, "f16": 2}
+
+
+class Rows(C.Structure):
+    """tad_rows: rows of contiguous elements of one type ("f32", "bf16", "f16"), `stride` elements apart."""
+    _fields_ = [("data", C.c_void_p), ("stride", C.c_int64), ("type", C.c_int32), ("reserved", C.c_int32)]
+
+    def __init__(self, ptr: int, stride: int, type: str):
+        super().__init__(ptr or None, stride, TYPE[type], 0)
+
+
+class Packed(C.Structure):
+    """tad_packed: e4m3 bytes and one exponent byte for each block of 128 of a row; strides in bytes."""
+    _fields_ = [("q", C.c_void_p), ("scale", C.c_void_p), ("q_stride", C.c_int64), ("scale_stride", C.c_int64)]
+
+    def __init__(self, q_ptr: int, scale_ptr: int, q_stride: int, scale_stride: int):
+        super().__init__(q_ptr or None, scale_ptr or None, q_stride, scale_stride)
+
+
 def _load() -> C.CDLL:
     if not os.path.exists(_LIB_PATH):
         raise ImportError(f"{_LIB_PATH} is missing: build it with paper_1711_01348_b200/build.py "
@@ -107,6 +129,20 @@ def _load() -> C.CDLL:
     lib.tad_smith_normal_form.argtypes = [i64p, C.c_int32, C.c_int32, i64p, i64p, i64p, i32p]
     lib.tad_fourier_motzkin.argtypes = [i64p, C.c_int32, C.c_int32, C.c_int32, i32p, i32p,
                                         i64p, i64p, i64p, i64p, i64p, i64p, i32p, i64p]
+    rows, packed, i64, i32, size, flt = C.POINTER(Rows), C.POINTER(Packed), C.c_int64, C.c_int32, C.c_size_t, C.c_float
+    lib.tad_pack8.argtypes = [rows, i64, i64, packed, vp]
+    lib.tad_unpack8.argtypes = [packed, i64, i64, rows, vp]
+    lib.tad_repack8.argtypes = [packed, i64, i64, packed, vp]
+    lib.tad_layernorm_forward.argtypes = [rows, i64, i64, rows, rows, flt, rows, vp, vp, packed, vp]
+    lib.tad_layernorm_workspace_bytes.argtypes = [i64, i64]
+    lib.tad_layernorm_backward.argtypes = [rows, rows, packed, i64, i64, rows, vp, vp, rows, rows, rows, vp, size, vp]
+    lib.tad_embed_forward.argtypes = [vp, i32, i64, rows, i64, i64, flt, rows, vp]
+    lib.tad_embed_workspace_bytes.argtypes = [i64, i64, i64]
+    lib.tad_embed_backward.argtypes = [vp, i32, i64, rows, i64, i64, flt, rows, i32, vp, size, vp]
+    lib.tad_matmul8_workspace_bytes.argtypes = [i64, i64, i64]
+    lib.tad_matmul8.argtypes = [packed, packed, i64, i64, i64, rows, vp, size, vp]
+    for name in ("tad_layernorm_workspace_bytes", "tad_embed_workspace_bytes", "tad_matmul8_workspace_bytes"):
+        getattr(lib, name).restype = size
     return lib
 
 
@@ -279,6 +315,64 @@ class Plan:
         buf = C.create_string_buffer(n)
         lib.tad_plan_print(self._h, which, a, i, buf, n)
         return buf.value.decode()
+
+
+# ---- operators of language models (pointers are integers, as above; None = not given) ----
+
+def pack8(x: Rows, n_rows: int, width: int, out: Packed, stream: int = 0) -> None:
+    _check(lib.tad_pack8(x, n_rows, width, out, stream or None))
+
+
+def unpack8(packed: Packed, n_rows: int, width: int, x: Rows, stream: int = 0) -> None:
+    _check(lib.tad_unpack8(packed, n_rows, width, x, stream or None))
+
+
+def repack8(packed: Packed, n_rows: int, width: int, out: Packed, stream: int = 0) -> None:
+    """The transpose of a packed n_rows x width matrix, packed anew."""
+    _check(lib.tad_repack8(packed, n_rows, width, out, stream or None))
+
+
+def layernorm_forward(x: Rows, n_rows: int, width: int, y: Rows, weight: Optional[Rows] = None, bias: Optional[Rows] = None,
+                      eps: float = 1e-5, mean_ptr: int = 0, rstd_ptr: int = 0, checkpoint: Optional[Packed] = None,
+                      stream: int = 0) -> None:
+    _check(lib.tad_layernorm_forward(x, n_rows, width, weight, bias, eps, y, mean_ptr or None, rstd_ptr or None, checkpoint,
+                                     stream or None))
+
+
+def layernorm_workspace_bytes(n_rows: int, width: int) -> int:
+    return int(lib.tad_layernorm_workspace_bytes(n_rows, width))
+
+
+def layernorm_backward(dy: Rows, x: Optional[Rows], checkpoint: Optional[Packed], n_rows: int, width: int, mean_ptr: int, rstd_ptr: int,
+                       dx: Optional[Rows] = None, weight: Optional[Rows] = None, dweight: Optional[Rows] = None,
+                       dbias: Optional[Rows] = None, workspace_ptr: int = 0, workspace_bytes: int = 0, stream: int = 0) -> None:
+    """From x or from its checkpoint: one of the two is None."""
+    _check(lib.tad_layernorm_backward(dy, x, checkpoint, n_rows, width, weight, mean_ptr or None, rstd_ptr or None, dx, dweight, dbias,
+                                      workspace_ptr or None, workspace_bytes, stream or None))
+
+
+def embed_forward(tokens_ptr: int, token_bits: int, n_tokens: int, table: Rows, n_table: int, width: int, factor: float, y: Rows,
+                  stream: int = 0) -> None:
+    _check(lib.tad_embed_forward(tokens_ptr or None, token_bits, n_tokens, table, n_table, width, factor, y, stream or None))
+
+
+def embed_workspace_bytes(n_tokens: int, n_table: int, width: int) -> int:
+    return int(lib.tad_embed_workspace_bytes(n_tokens, n_table, width))
+
+
+def embed_backward(tokens_ptr: int, token_bits: int, n_tokens: int, dy: Rows, n_table: int, width: int, factor: float, dtable: Rows,
+                   accumulate: bool = False, workspace_ptr: int = 0, workspace_bytes: int = 0, stream: int = 0) -> None:
+    _check(lib.tad_embed_backward(tokens_ptr or None, token_bits, n_tokens, dy, n_table, width, factor, dtable, int(accumulate),
+                                  workspace_ptr or None, workspace_bytes, stream or None))
+
+
+def matmul8_workspace_bytes(m: int, n: int, k: int) -> int:
+    return int(lib.tad_matmul8_workspace_bytes(m, n, k))
+
+
+def matmul8(a: Packed, b: Packed, m: int, n: int, k: int, y: Rows, workspace_ptr: int = 0, workspace_bytes: int = 0, stream: int = 0) -> None:
+    """y = a b^T of packed matrices, a m x k and b n x k."""
+    _check(lib.tad_matmul8(a, b, m, n, k, y, workspace_ptr or None, workspace_bytes, stream or None))
 
 
 # ---- host-only pieces of the integer algebra (for tests) ----
