@@ -3,11 +3,18 @@
 //     mean = sum x / D,  rstd = (sum (x - mean)^2 / D + eps)^(-1/2),  xh = (x - mean) rstd,  y = xh w + b
 //     g = dy w,  dx = rstd (g - sum g / D - xh sum (g xh) / D),  dw = sum_rows dy xh,  db = sum_rows dy
 //
-// Both passes read every element once and are bound by memory.  A row is held in registers, sixteen elements a thread, by a warp
-// (up to 512 columns) or a block, which walks over the rows that are its share with the next row's loads under way; the
-// variance is the mean of the squared deviations of those registers (no difference of large sums).  Weights stay in registers
-// over all rows.  The backward pass keeps its share of dw and db there too and writes them once, as a plane of partial
-// sums; a second kernel adds the planes up in a fixed order.  Rows longer than a block holds are read twice or three times.
+// Both passes read every element once and are bound by memory.  A row is held in registers, sixteen elements a thread, by a group of
+// 1 to 16 warps or, in longer rows, by a cluster of such groups; a group walks over the rows that are its share.  Rows of
+// whole 16-byte pieces come by bulk copies into a ring of shared memory, two to four rows ahead (32 KB of rows under way a block of the
+// forward pass, 128 KB of the backward pass): prefetched into registers instead they take those that a second and third block
+// an SM need (8192 x 4096 fp32, forward / backward: 51 / 83 us).  Other rows are loaded an element at a time, one row ahead.  The
+// variance is the mean of the squared deviations of the registers (no difference of large sums).  Weights stay in registers
+// over all rows.  The backward pass keeps its share of dw and db there too and writes them once a block, as a plane of partial
+// sums; a second kernel adds the planes up in a fixed order.  Rows longer than a cluster holds are read twice or three times.
+#include <cooperative_groups.h>
+
+#include <atomic>
+
 #include "rows.cuh"
 
 tad_status tad_launch_pack8(const tad_rows *x, int64_t n_rows, int64_t width, const tad_packed *out, cudaStream_t stream);
@@ -15,11 +22,16 @@ tad_status tad_launch_pack8(const tad_rows *x, int64_t n_rows, int64_t width, co
 namespace {
 
 using namespace tadr;
+namespace cg = cooperative_groups;
 
-constexpr int E = 16;                      // elements of a row in a thread's registers
-constexpr int WARP_WIDTH = 32 * E;         // rows that a warp holds
-constexpr int SMALL = 256, LARGE = 1024;   // threads of a block: with and without the weights in registers
-constexpr int HELD = LARGE * E;            // longest row that a block holds
+// Threads of a block: forward 256, three blocks an SM (80 registers a thread); backward 512, one (128).  Elements of a row in a thread's
+// registers (E): sixteen; eight where the backward pass loads single elements, whose next row lies in registers as well (with sixteen they
+// spill, and what is spilled is waited for at once: 5003 x 1001 fp32 22 us for 17).
+constexpr int FORWARD_BLOCK = 256, FORWARD_BLOCKS = 3, BACKWARD_BLOCK = 512, FORWARD_E = 16;
+template <int V> constexpr int BACKWARD_E = V == 8 ? 16 : 8;
+constexpr int MAX_CLUSTER = 8;
+constexpr int HELD = FORWARD_BLOCK * FORWARD_E * MAX_CLUSTER;      // longest row that a cluster holds
+constexpr int LARGE = 1024, SMALL = 256;   // threads of a block of the kernels for longer rows
 
 // source type of a packed matrix
 struct Packed8 {};
@@ -33,141 +45,469 @@ struct Params {
     float *mean, *rstd, *planes;
     int64_t n_rows;
     int width, w_type, b_type, y_type, dx_type;
+    int group;                             // threads of a group
     float eps, inv_width;
 };
 
-// sums of two values over the warp or, `warps` > 1, over the block: the same bits in every thread
-__device__ __forceinline__ float2 warp_sum(float2 v)
-{
-#pragma unroll
-    for (int d = 16; d; d >>= 1) { v.x += __shfl_xor_sync(0xffffffffu, v.x, d); v.y += __shfl_xor_sync(0xffffffffu, v.y, d); }
-    return v;
-}
-// `box`: 2 x 32 places used in turn, so that one barrier a sum is enough
-struct Sum {
-    float2 (*box)[32];
-    int turn;
-    template <bool WARP>
-    __device__ __forceinline__ float2 of(float2 v)
+// How rows are divided: a warp a row, a group of warps, a cluster of groups (a block each).
+enum { BY_WARP, BY_GROUP, BY_CLUSTER };
+
+// A thread's E elements lie in the 32 E columns of its warp: V = 8, pieces of eight, 256 columns apart; V = 16, two of them side by side;
+// V = 1, 32 apart.  So every access of a row is the thread's pointer and a constant.  Piece i exists where place(i) < rem, the columns
+// from the thread's first one to the end of the row.
+template <int V> struct Of {
+    static constexpr int PIECE = V == 1 ? 1 : 8;
+    __device__ __forceinline__ static constexpr int place(int i) { return V == 16 ? i * 8 : V == 8 ? i * 256 : i * 32; }
+    // column of element e behind the thread's first
+    __device__ __forceinline__ static constexpr int column(int e) { return place(e / PIECE) + e % PIECE; }
+};
+
+template <class T, int V, int E>
+struct Held {
+    static constexpr int PV = Of<V>::PIECE;
+    Piece<T, PV> p[E / PV];
+    __device__ __forceinline__ void zero()
     {
-        v = warp_sum(v);
-        if (WARP) return v;
-        const int warps = blockDim.x >> 5, lane = threadIdx.x & 31;
-        if (lane == 0) box[turn][threadIdx.x >> 5] = v;
-        __syncthreads();
-        v = lane < warps ? box[turn][lane] : make_float2(0.f, 0.f);
-        turn ^= 1;
-        return warp_sum(v);
+#pragma unroll
+        for (int i = 0; i < E / PV; ++i) p[i].zero();
+    }
+    // (pieces that do not exist keep their zeros)
+    __device__ __forceinline__ void fetch(const T *__restrict__ at, int rem)
+    {
+#pragma unroll
+        for (int i = 0; i < E / PV; ++i) if (Of<V>::place(i) < rem) p[i].load(at + Of<V>::place(i));
+    }
+    __device__ __forceinline__ void get(float (&v)[E]) const
+    {
+#pragma unroll
+        for (int i = 0; i < E / PV; ++i) {
+            float f[PV];
+            p[i].get(f);
+#pragma unroll
+            for (int j = 0; j < PV; ++j) v[i * PV + j] = f[j];
+        }
     }
 };
 
-// V elements of the vector `p` from column c on (zero behind the row)
-template <int V>
-__device__ __forceinline__ void load_vector(float (&v)[V], const void *p, int type, int c, int width, float none)
+// E elements of a vector whose type is known at run time; behind the row zeros
+template <class T, int V, int E>
+__device__ __forceinline__ void load_held(float (&v)[E], const T *p, int rem)
 {
+    Held<T, V, E> h;
+    h.zero();
+    h.fetch(p, rem);
+    h.get(v);
+}
+template <int V, int E>
+__device__ __forceinline__ void load_vector(float (&v)[E], const void *p, int type, int c, int rem, float none)
+{
+    if (!p) {
 #pragma unroll
-    for (int j = 0; j < V; ++j) v[j] = !p ? none : c + j < width ? element(p, type, c + j) : 0.f;
+        for (int e = 0; e < E; ++e) v[e] = none;
+    } else if (V != 1 && reinterpret_cast<uintptr_t>(p) % 16 != 0) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[e] = Of<V>::place(e / Of<V>::PIECE) < rem ? element(p, type, c + Of<V>::column(e)) : 0.f;
+    } else if (type == TAD_F32) load_held<float, V, E>(v, static_cast<const float *>(p) + c, rem);
+    else if (type == TAD_BF16) load_held<__nv_bfloat16, V, E>(v, static_cast<const __nv_bfloat16 *>(p) + c, rem);
+    else load_held<__half, V, E>(v, static_cast<const __half *>(p) + c, rem);
 }
 
-template <int V>
-__device__ __forceinline__ void store_typed(void *base, int type, int64_t at, const float (&v)[V])
+template <class O, int V, int E>
+__device__ __forceinline__ void store_held(O *at, int rem, const float (&v)[E])
 {
-    if (type == TAD_F32) { Piece<float, V> o; o.set(v); o.store(static_cast<float *>(base) + at); }
-    else if (type == TAD_BF16) { Piece<__nv_bfloat16, V> o; o.set(v); o.store(static_cast<__nv_bfloat16 *>(base) + at); }
-    else { Piece<__half, V> o; o.set(v); o.store(static_cast<__half *>(base) + at); }
+    constexpr int PV = Of<V>::PIECE;
+#pragma unroll
+    for (int i = 0; i < E / PV; ++i) {
+        if (Of<V>::place(i) >= rem) continue;
+        float f[PV];
+#pragma unroll
+        for (int j = 0; j < PV; ++j) f[j] = v[i * PV + j];
+        Piece<O, PV> o;
+        o.set(f);
+        o.store(at + Of<V>::place(i));
+    }
+}
+template <int V, int E>
+__device__ __forceinline__ void store_typed(void *base, int type, int64_t at, int rem, const float (&v)[E])
+{
+    if (type == TAD_F32) store_held<float, V, E>(static_cast<float *>(base) + at, rem, v);
+    else if (type == TAD_BF16) store_held<__nv_bfloat16, V, E>(static_cast<__nv_bfloat16 *>(base) + at, rem, v);
+    else store_held<__half, V, E>(static_cast<__half *>(base) + at, rem, v);
+}
+
+// two elements by one instruction (elements 2 j and 2 j + 1 of a thread)
+template <int E> struct Pairs {
+    float2 p[E / 2];
+    __device__ __forceinline__ void set(const float (&v)[E])
+    {
+#pragma unroll
+        for (int j = 0; j < E / 2; ++j) p[j] = make_float2(v[2 * j], v[2 * j + 1]);
+    }
+    __device__ __forceinline__ void get(float (&v)[E]) const
+    {
+#pragma unroll
+        for (int j = 0; j < E / 2; ++j) { v[2 * j] = p[j].x; v[2 * j + 1] = p[j].y; }
+    }
+};
+// a value of the pieces that exist, zero behind the row, for elements 2 j and 2 j + 1
+template <int V> __device__ __forceinline__ float2 inside(float v, int j, int rem)
+{
+    return make_float2(Of<V>::place(2 * j / Of<V>::PIECE) < rem ? v : 0.f, Of<V>::place((2 * j + 1) / Of<V>::PIECE) < rem ? v : 0.f);
+}
+
+__device__ __forceinline__ float warp_sum(float v)
+{
+#pragma unroll
+    for (int d = 16; d; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+    return v;
+}
+
+constexpr long long WAIT_LIMIT = 1ll << 31;        // clocks (about a second) after which a wait gives up
+__device__ __forceinline__ bool wait_once(unsigned bar, unsigned parity)
+{
+    unsigned ok;
+    asm volatile("{ .reg .pred p; mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return ok != 0;
+}
+__device__ __forceinline__ bool wait_for(unsigned bar, unsigned parity)
+{
+    if (wait_once(bar, parity)) return true;
+    const long long begin = clock64();
+    while (clock64() - begin < WAIT_LIMIT) if (wait_once(bar, parity)) return true;
+    return false;
+}
+
+// What the blocks of a cluster tell each other: each one's sums go into everybody's shared memory by stores that count at the
+// receiver's mbarrier.  (A cluster barrier instead would wait, as a release, for the rows just written: 8192 columns forward 55 us
+// for 28.)
+template <int N>
+struct Exchange {
+    float far[2][MAX_CLUSTER][N];
+    unsigned long long bar[2];
+};
+// Sums of N values over all threads that share a row, the same bits in each of them.  A warp's sum goes into a box of shared
+// memory, everybody adds the boxes up in order; two sets of boxes are used in turn, so one barrier a sum is enough.  ALONE: the group
+// is the block.
+template <int N, int BY, bool ALONE>
+struct Sum {
+    float (*box)[BACKWARD_BLOCK / 32][N];  // [2], of this block
+    Exchange<N> *ex;
+    int first, warps, id, threads;         // this group: its first warp, its warps, its barrier and its threads
+    int count;                             // sums so far
+    unsigned blocks, rank;                 // of the cluster
+    bool lost;                             // a wait has run out, there are no further ones
+    __device__ __forceinline__ void start()
+    {
+        if (BY != BY_CLUSTER) return;
+        cg::cluster_group cluster = cg::this_cluster();
+        blocks = cluster.num_blocks();
+        rank = cluster.block_rank();
+        if (threadIdx.x == 0) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"((unsigned)__cvta_generic_to_shared(&ex->bar[i])) : "memory");
+            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        }
+        cluster.sync();
+    }
+    __device__ __forceinline__ void of(float (&v)[N])
+    {
+        const int turn = count & 1;
+        if (BY == BY_WARP) {
+#pragma unroll
+            for (int k = 0; k < N; ++k) v[k] = warp_sum(v[k]);
+            return;
+        }
+        // two values in five steps: the halves of the warp trade one for the other and go on with one each
+        const int lane = threadIdx.x & 31, mine = N == 2 ? lane >> 4 : 0;
+        float a = N == 2 && mine ? v[N - 1] : v[0];
+        a += __shfl_xor_sync(0xffffffffu, N == 2 && !mine ? v[N - 1] : v[0], 16);
+#pragma unroll
+        for (int d = 8; d; d >>= 1) a += __shfl_xor_sync(0xffffffffu, a, d);
+        if (lane % (32 / N) == 0) box[turn][threadIdx.x >> 5][mine] = a;
+        // (barriers with a number known at run time only count as all sixteen of a block: four blocks an SM)
+        if (ALONE) __syncthreads();
+        else asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
+#pragma unroll
+        for (int k = 0; k < N; ++k) v[k] = 0.f;
+#pragma unroll
+        for (int w = 0; w < BACKWARD_BLOCK / 32; w += 2) {         // (groups have an even number of warps)
+            if (w >= warps) break;
+            if (N == 2) {
+                const float4 p = *reinterpret_cast<const float4 *>(&box[turn][first + w][0]);
+                v[0] += p.x + p.z;
+                v[N - 1] += p.y + p.w;
+            } else {
+                const float2 p = *reinterpret_cast<const float2 *>(&box[turn][first + w][0]);
+                v[0] += p.x + p.y;
+            }
+        }
+        if (BY == BY_CLUSTER) {
+            // (a block writes its sum n + 2 behind its sum n + 1, which waits for everybody's, sent behind the reads of sum n)
+            const unsigned bar = (unsigned)__cvta_generic_to_shared(&ex->bar[turn]);
+            if (threadIdx.x == 0) asm volatile("{ .reg .b64 t; mbarrier.arrive.expect_tx.shared::cta.b64 t, [%0], %1; }" ::"r"(bar), "r"(blocks * N * 4) : "memory");
+            if (threadIdx.x < blocks) {
+                unsigned to, at;
+                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"((unsigned)__cvta_generic_to_shared(&ex->far[turn][rank][0])), "r"(threadIdx.x));
+                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(bar), "r"(threadIdx.x));
+#pragma unroll
+                for (int k = 0; k < N; ++k)
+                    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.b32 [%0], %1, [%2];" ::"r"(to + 4 * k), "r"(__float_as_uint(v[k])), "r"(at) : "memory");
+            }
+            const unsigned parity = (count >> 1) & 1;
+            if (!lost) lost = !wait_for(bar, parity);
+#pragma unroll
+            for (int k = 0; k < N; ++k) {
+                float a = !lost ? 0.f : __uint_as_float(0x7fffffffu);         // (a block that never answered: no result)
+                for (unsigned b = 0; b < blocks; ++b) a += ex->far[turn][b][k];
+                v[k] = a;
+            }
+        }
+        ++count;
+    }
+    // no block leaves while another one may still write into it
+    __device__ __forceinline__ void finish() { if (BY == BY_CLUSTER) cg::this_cluster().sync(); }
+};
+
+// this thread's place: its group in the grid, the groups of the grid, its first column
+template <int BY, int V, int E>
+struct Place {
+    int64_t row, step;
+    int group, in;                         // the group in the block, the thread in the group
+    int col0, col, rem;                    // first column of the block and of the thread; columns from there to the end of the row
+    __device__ __forceinline__ Place(const Params &P)
+    {
+        const int groups = BY == BY_CLUSTER ? 1 : blockDim.x / P.group;
+        group = BY == BY_CLUSTER ? 0 : threadIdx.x / P.group;
+        in = threadIdx.x - group * P.group;
+        if (BY == BY_CLUSTER) {
+            cg::cluster_group cluster = cg::this_cluster();
+            const unsigned n = cluster.num_blocks();
+            row = blockIdx.x / n;
+            step = gridDim.x / n;
+            col0 = (int)(cluster.block_rank() * blockDim.x) * E;
+        } else {
+            row = (int64_t)blockIdx.x * groups + group;
+            step = (int64_t)gridDim.x * groups;
+            col0 = 0;
+        }
+        col = col0 + (in >> 5) * (32 * E) + (in & 31) * V;
+        rem = P.width - col;
+    }
+};
+
+template <int N, int BY, bool ALONE>
+__device__ __forceinline__ Sum<N, BY, ALONE> sum_of(const Params &P, float (*box)[BACKWARD_BLOCK / 32][N], Exchange<N> *ex)
+{
+    const int g = BY == BY_CLUSTER ? 0 : threadIdx.x / P.group;
+    Sum<N, BY, ALONE> s{box, ex, g * (P.group >> 5), P.group >> 5, 1 + g, P.group, 0, 1, 0, false};
+    s.start();
+    return s;
+}
+
+// ---- rows ahead ----
+
+__device__ __forceinline__ unsigned smem_u32(const void *p) { return (unsigned)__cvta_generic_to_shared(p); }
+
+// The ring of a group: STAGES rows (of a block's columns) of up to two tensors, a barrier a stage that counts their bytes.  The group's first
+// thread issues the copies.
+template <int STAGES>
+struct Ring {
+    unsigned buf, bars, stage_bytes;       // this group's rows (offset in `rows`) and barriers
+    unsigned char *rows;
+    bool leader, lost;                     // lost: a wait has run out, there are no further waits and copies
+    int at;                                // the stage of the next row
+    unsigned parity;
+    __device__ __forceinline__ void start(unsigned char *smem, unsigned offset, unsigned bar, unsigned bytes, bool first)
+    {
+        rows = smem; buf = offset; bars = bar; stage_bytes = bytes; leader = first; lost = false; at = 0; parity = 0;
+        if (leader) {
+#pragma unroll
+            for (int i = 0; i < STAGES; ++i) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bars + 8 * i) : "memory");
+            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+            asm volatile("fence.proxy.async.global;" ::: "memory");          // (the rows are another kernel's plain stores)
+        }
+    }
+    // by the leader: a row's bytes of a tensor into stage `i` at `offset`; expect() first, with the bytes of all of them
+    __device__ __forceinline__ void expect(int i, unsigned bytes)
+    {
+        asm volatile("{ .reg .b64 t; mbarrier.arrive.expect_tx.shared::cta.b64 t, [%0], %1; }" ::"r"(bars + 8 * i), "r"(bytes) : "memory");
+    }
+    __device__ __forceinline__ void copy(int i, unsigned offset, const void *from, unsigned bytes)
+    {
+        if (bytes) asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_u32(rows) + buf + i * stage_bytes + offset), "l"(from), "r"(bytes), "r"(bars + 8 * i) : "memory");
+    }
+    // waits for the row at the ring's head (a second at most)
+    __device__ __forceinline__ bool wait()
+    {
+        if (!lost) lost = !wait_for(bars + 8 * at, parity);
+        return !lost;
+    }
+    __device__ __forceinline__ const unsigned char *row() const { return rows + buf + at * stage_bytes; }
+    __device__ __forceinline__ void advance() { if (++at == STAGES) { at = 0; parity ^= 1; } }
+};
+
+// The thread's elements of a row in the ring.  Every thread reads its places, whether they exist or not: those behind the row hold zeros
+// from the start (clear_ring), which costs no selects where the row is read.
+template <class T, int E, int V = 8>
+__device__ __forceinline__ void read_row(Piece<T, 8> (&p)[E / 8], const T *at)
+{
+#pragma unroll
+    for (int i = 0; i < E / 8; ++i) p[i].load(at + Of<V>::place(i));
+}
+template <class T, int E>
+__device__ __forceinline__ void elements(float (&v)[E], const Piece<T, 8> (&p)[E / 8])
+{
+#pragma unroll
+    for (int i = 0; i < E / 8; ++i) {
+        float f[8];
+        p[i].get(f);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[i * 8 + j] = f[j];
+    }
+}
+// by the whole block, before the first copy; a barrier follows
+__device__ __forceinline__ void clear_ring(unsigned char *rows, unsigned bytes)
+{
+    for (unsigned i = threadIdx.x * 16; i < bytes; i += blockDim.x * 16) *reinterpret_cast<uint4 *>(rows + i) = make_uint4(0, 0, 0, 0);
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");             // (the copies write the same places)
 }
 
 // ---- forward ----
 
-// V = 8: width and all row starts are whole pieces of eight.  HOLD: the weights stay in registers.  KEEP: x goes into 8 bits
-// beside the pass (V = 8: sixteen neighbouring threads hold a block of 128).
-template <class T, int V, bool WARP, bool HOLD, bool KEEP>
-__global__ void __launch_bounds__(HOLD ? SMALL : LARGE, HOLD ? 3 : 1)
-tad_norm_forward_kernel(const Params P)
+template <class T> constexpr int FORWARD_STAGES = sizeof(T) == 2 ? 4 : 2;
+
+// x into 8 bits beside the pass.  16-bit types (V = 16): eight neighbouring threads hold a block of 128, sixteen elements each; fp32 (V = 8):
+// sixteen threads.
+template <class T, int V>
+__device__ __forceinline__ void keep_row(const Params &P, int64_t r, int col, int rem, const Piece<T, 8> (&p)[2])
 {
-    constexpr int NV = E / V;
-    __shared__ float2 box[2][32];
-    tad_wait_previous();
-    Sum sum{box, 0};
-    const int tid = WARP ? threadIdx.x & 31 : threadIdx.x, span = WARP ? 32 : blockDim.x;
-    const int64_t step = WARP ? (int64_t)gridDim.x * (SMALL / 32) : gridDim.x;
-    int64_t r = WARP ? (int64_t)blockIdx.x * (SMALL / 32) + (threadIdx.x >> 5) : blockIdx.x;
-    const T *__restrict__ x = static_cast<const T *>(P.x);
-    const int width = P.width;
-    float w[HOLD ? NV : 1][V], b[HOLD ? NV : 1][V];
-    if constexpr (HOLD) {
+    if constexpr (V == 16) {
+        Sixteen<T> x;
+        const unsigned w[8] = {p[0].a.x, p[0].a.y, p[0].a.z, p[0].a.w, p[1].a.x, p[1].a.y, p[1].a.z, p[1].a.w};
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int c = (i * span + tid) * V;
-            load_vector<V>(w[i], P.w, P.w_type, c, width, 1.f);
-            load_vector<V>(b[i], P.b, P.b_type, c, width, 0.f);
+        for (int j = 0; j < 8; ++j) x.w[j] = w[j];
+        unsigned byte;
+        const uint4 q = x.pack(byte);
+        uint8_t *to = P.kq + r * P.kqs + col;
+        if (rem > 8) *reinterpret_cast<uint4 *>(to) = q;
+        else if (rem > 0) *reinterpret_cast<uint2 *>(to) = make_uint2(q.x, q.y);
+        if ((threadIdx.x & 7) == 0 && rem > 0) P.kscale[r * P.kss + col / TAD_BLOCK8] = (uint8_t)byte;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            float f[8];
+            p[i].get(f);
+            unsigned byte;
+            const uint2 q = pack_block(f, byte);
+            if (Of<V>::place(i) >= rem) continue;
+            const int c = col + Of<V>::place(i);
+            *reinterpret_cast<uint2 *>(P.kq + r * P.kqs + c) = q;
+            if ((threadIdx.x & 15) == 0) P.kscale[r * P.kss + c / TAD_BLOCK8] = (uint8_t)byte;
         }
     }
-    Piece<T, V> next[NV];
-    auto fetch = [&](int64_t row) {
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int c = (i * span + tid) * V;
-            next[i].zero();
-            if (row < P.n_rows && c < width) next[i].load(x + row * P.xs + c);
+}
+
+// V = 8, 16: width and all row starts are whole pieces of eight.  KEEP: with the checkpoint.
+template <class T, int V, int BY, bool KEEP>
+__global__ void __launch_bounds__(FORWARD_BLOCK, V == 1 ? 2 : FORWARD_BLOCKS)
+tad_norm_forward_kernel(const Params P)
+{
+    constexpr int E = FORWARD_E, STAGES = FORWARD_STAGES<T>;
+    __shared__ __align__(16) float box[2][BACKWARD_BLOCK / 32][1];
+    __shared__ Exchange<1> ex;
+    __shared__ unsigned long long bars[FORWARD_BLOCK / 32][STAGES];
+    extern __shared__ __align__(128) unsigned char rows[];
+    tad_wait_previous();
+    Sum<1, BY, true> sum = sum_of<1, BY, true>(P, box, &ex);
+    const Place<BY, V, E> at(P);
+    int64_t r = at.row;
+    const T *__restrict__ x = static_cast<const T *>(P.x);
+    Held<T, 1, V == 1 ? E : 1> next;       // (V = 1)
+    Ring<STAGES> ring;
+    const unsigned bytes = (unsigned)max(0, min(P.width - at.col0, P.group * E)) * (unsigned)sizeof(T);
+    if constexpr (V != 1) {
+        ring.start(rows, at.group * STAGES * P.group * E * (unsigned)sizeof(T), smem_u32(&bars[at.group][0]), P.group * E * (unsigned)sizeof(T), at.in == 0);
+        clear_ring(rows, blockDim.x * STAGES * E * (unsigned)sizeof(T));
+        __syncthreads();
+        if (ring.leader)
+            for (int i = 0; i < STAGES; ++i)
+                if (r + i * at.step < P.n_rows) {
+                    ring.expect(i, bytes);
+                    ring.copy(i, 0, x + (r + i * at.step) * P.xs + at.col0, bytes);
+                }
+    } else {
+        next.zero();
+        if (r < P.n_rows) next.fetch(x + r * P.xs + at.col, at.rem);
+    }
+    Pairs<E> w, b;
+    {
+        float f[E];
+        load_vector<V, E>(f, P.w, P.w_type, at.col, at.rem, 1.f);
+        w.set(f);
+        load_vector<V, E>(f, P.b, P.b_type, at.col, at.rem, 0.f);
+        b.set(f);
+    }
+    for (; r < P.n_rows; r += at.step) {
+        float v[E];
+        if constexpr (V != 1) {
+            ring.wait();
+            Piece<T, 8> p[E / 8];
+            read_row<T, E, V>(p, reinterpret_cast<const T *>(ring.row()) + (at.col - at.col0));
+            elements<T, E>(v, p);
+            if constexpr (KEEP) keep_row<T, V>(P, r, at.col, at.rem, p);
+        } else {
+            next.get(v);
+            if (r + at.step < P.n_rows) next.fetch(x + (r + at.step) * P.xs + at.col, at.rem);
         }
-    };
-    fetch(r);
-    for (; r < P.n_rows; r += step) {
-        float v[NV][V];
-        float total = 0.f;
+        Pairs<E> u;
+        u.set(v);
+        float2 two = u.p[0];
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            next[i].get(v[i]);
-#pragma unroll
-            for (int j = 0; j < V; ++j) total += v[i][j];
-        }
-        fetch(r + step);
-        const float mean = sum.template of<WARP>(make_float2(total, 0.f)).x * P.inv_width;
-        if constexpr (KEEP) {
-#pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                const int c = (i * span + tid) * V;
-                float a = 0.f;
-#pragma unroll
-                for (int j = 0; j < V; ++j) a = fmaxf(a, finite_abs(v[i][j]));
-#pragma unroll
-                for (int d = 8; d; d >>= 1) a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, d));
-                if (c >= width) continue;
-                const unsigned s = scale_byte(a);
-                if constexpr (V == 8) *reinterpret_cast<uint2 *>(P.kq + r * P.kqs + c) = pack_eight(v[i], inverse_scale(s));
-                if ((tid & 15) == 0) P.kscale[r * P.kss + c / TAD_BLOCK8] = (uint8_t)s;
+        for (int j = 1; j < E / 2; ++j) two = __fadd2_rn(two, u.p[j]);
+        float s[1] = {two.x + two.y};
+        sum.of(s);
+        if constexpr (V != 1) {
+            // (behind the sum every thread of the group has read the row)
+            if (ring.leader && !ring.lost && r + STAGES * at.step < P.n_rows) {
+                ring.expect(ring.at, bytes);
+                ring.copy(ring.at, 0, x + (r + STAGES * at.step) * P.xs + at.col0, bytes);
             }
+            ring.advance();
         }
-        float squares = 0.f;
+        // (a row that never came has no result)
+        const float mean = V != 1 && ring.lost ? __uint_as_float(0x7fffffffu) : s[0] * P.inv_width;
+        two = make_float2(0.f, 0.f);
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const bool live = (i * span + tid) * V < width;
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-                v[i][j] -= mean;
-                if (live) squares += v[i][j] * v[i][j];
-            }
+        for (int j = 0; j < E / 2; ++j) {
+            u.p[j] = __fadd2_rn(u.p[j], inside<V>(-mean, j, at.rem));        // (zeros behind the row deviate by nothing)
+            two = __ffma2_rn(u.p[j], u.p[j], two);
         }
-        const float rstd = rsqrtf(sum.template of<WARP>(make_float2(squares, 0.f)).x * P.inv_width + P.eps);
-        if (tid == 0) {
+        s[0] = two.x + two.y;
+        sum.of(s);
+        const float rstd = rsqrtf(s[0] * P.inv_width + P.eps);
+        if (at.col == 0) {
             if (P.mean) P.mean[r] = mean;
             if (P.rstd) P.rstd[r] = rstd;
         }
+        const float2 rr = make_float2(rstd, rstd);
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int c = (i * span + tid) * V;
-            if (c >= width) continue;
-            float o[V], wr[V], br[V];
-            if constexpr (!HOLD) {
-                load_vector<V>(wr, P.w, P.w_type, c, width, 1.f);
-                load_vector<V>(br, P.b, P.b_type, c, width, 0.f);
-            }
-#pragma unroll
-            for (int j = 0; j < V; ++j) o[j] = fmaf(v[i][j] * rstd, HOLD ? w[HOLD ? i : 0][j] : wr[j], HOLD ? b[HOLD ? i : 0][j] : br[j]);
-            store_typed<V>(P.y, P.y_type, r * P.ys + c, o);
-        }
+        for (int j = 0; j < E / 2; ++j) u.p[j] = __ffma2_rn(__fmul2_rn(u.p[j], rr), w.p[j], b.p[j]);
+        u.get(v);
+        store_typed<V, E>(P.y, P.y_type, r * P.ys + at.col, at.rem, v);
     }
+    sum.finish();
+}
+
+// of one value over a block of 1024 threads
+template <int N>
+__device__ __forceinline__ float block_sum(float v, float (*box)[N][32], int &turn, int k)
+{
+    v = warp_sum(v);
+    if ((threadIdx.x & 31) == 0) box[turn][k][threadIdx.x >> 5] = v;
+    __syncthreads();
+    v = warp_sum(box[turn][k][threadIdx.x & 31]);
+    turn ^= 1;
+    return v;
 }
 
 // rows of any length: three passes over the row, the second and third from L2
@@ -175,19 +515,19 @@ template <class T>
 __global__ void __launch_bounds__(LARGE)
 tad_norm_forward_long_kernel(const Params P)
 {
-    __shared__ float2 box[2][32];
+    __shared__ float box[2][1][32];
     tad_wait_previous();
-    Sum sum{box, 0};
+    int turn = 0;
     for (int64_t r = blockIdx.x; r < P.n_rows; r += gridDim.x) {
         const T *__restrict__ x = static_cast<const T *>(P.x) + r * P.xs;
         float a = 0.f;
 #pragma unroll 8
         for (int c = threadIdx.x; c < P.width; c += LARGE) a += to_float(x[c]);
-        const float mean = sum.of<false>(make_float2(a, 0.f)).x * P.inv_width;
+        const float mean = block_sum(a, box, turn, 0) * P.inv_width;
         a = 0.f;
 #pragma unroll 8
         for (int c = threadIdx.x; c < P.width; c += LARGE) { const float d = to_float(x[c]) - mean; a += d * d; }
-        const float rstd = rsqrtf(sum.of<false>(make_float2(a, 0.f)).x * P.inv_width + P.eps);
+        const float rstd = rsqrtf(block_sum(a, box, turn, 0) * P.inv_width + P.eps);
         if (threadIdx.x == 0) {
             if (P.mean) P.mean[r] = mean;
             if (P.rstd) P.rstd[r] = rstd;
@@ -211,18 +551,6 @@ struct Source {
     __device__ __forceinline__ void get(float (&v)[V]) const { p.get(v); }
 };
 template <>
-struct Source<Packed8, 8> {
-    uint2 q;
-    unsigned s;
-    __device__ __forceinline__ void zero() { q = make_uint2(0, 0); s = 127; }
-    __device__ __forceinline__ void load(const Params &P, int64_t r, int c)
-    {
-        q = *reinterpret_cast<const uint2 *>(P.q + r * P.qs + c);
-        s = P.scale[r * P.ss + c / TAD_BLOCK8];
-    }
-    __device__ __forceinline__ void get(float (&v)[8]) const { unpack_eight(q, scale_of(s), v); }
-};
-template <>
 struct Source<Packed8, 1> {
     uint8_t q, s;
     __device__ __forceinline__ void zero() { q = 0; s = 127; }
@@ -230,108 +558,198 @@ struct Source<Packed8, 1> {
     __device__ __forceinline__ void get(float (&v)[1]) const { v[0] = from_e4m3x2(q).x * scale_of(s); }
 };
 
-template <class S, class T, int V, bool WARP, bool HOLD>
-__global__ void __launch_bounds__(HOLD ? SMALL : LARGE, HOLD ? 2 : 1)
+// V = 1: the thread's elements of the next row of the input
+template <class S, int E>
+struct HeldSource {
+    Held<S, 1, E> h;
+    __device__ __forceinline__ void zero() { h.zero(); }
+    __device__ __forceinline__ void fetch(const Params &P, int64_t r, int col, int rem) { h.fetch(static_cast<const S *>(P.x) + r * P.xs + col, rem); }
+    __device__ __forceinline__ void get(float (&v)[E]) const { h.get(v); }
+};
+template <int E>
+struct HeldSource<Packed8, E> {
+    Source<Packed8, 1> p[E];
+    __device__ __forceinline__ void zero()
+    {
+#pragma unroll
+        for (int i = 0; i < E; ++i) p[i].zero();
+    }
+    __device__ __forceinline__ void fetch(const Params &P, int64_t r, int col, int rem)
+    {
+#pragma unroll
+        for (int i = 0; i < E; ++i) if (Of<1>::place(i) < rem) p[i].load(P, r, col + Of<1>::place(i));
+    }
+    __device__ __forceinline__ void get(float (&v)[E]) const
+    {
+#pragma unroll
+        for (int i = 0; i < E; ++i) { float f[1]; p[i].get(f); v[i] = f[0]; }
+    }
+};
+
+// V = 8: bytes of an element in memory
+template <class S> constexpr int SOURCE_BYTES = sizeof(S);
+template <> constexpr int SOURCE_BYTES<Packed8> = 1;
+template <class S, class T> constexpr int BACKWARD_STAGES = SOURCE_BYTES<S> + (int)sizeof(T) <= 4 ? 4 : 2;
+
+template <class S, class T, int V, int BY>
+__global__ void __launch_bounds__(BACKWARD_BLOCK, 1)
 tad_norm_backward_kernel(const Params P)
 {
-    constexpr int NV = E / V;
-    __shared__ float2 box[2][32];
-    __shared__ float join[WARP ? SMALL / 32 : 1][WARP ? 32 * V : 1];
+    constexpr int E = BACKWARD_E<V>, STAGES = BACKWARD_STAGES<S, T>;
+    __shared__ __align__(16) float box[2][BACKWARD_BLOCK / 32][2];
+    __shared__ Exchange<2> ex;
+    __shared__ unsigned long long bars[BACKWARD_BLOCK / 32][STAGES];
+    extern __shared__ __align__(128) unsigned char rows[];
+    __shared__ __align__(16) float join[BY == BY_CLUSTER ? 1 : BACKWARD_BLOCK][BY == BY_CLUSTER ? 4 : 8];
     tad_wait_previous();
-    Sum sum{box, 0};
-    const int tid = WARP ? threadIdx.x & 31 : threadIdx.x, span = WARP ? 32 : blockDim.x;
-    const int64_t step = WARP ? (int64_t)gridDim.x * (SMALL / 32) : gridDim.x;
-    int64_t r = WARP ? (int64_t)blockIdx.x * (SMALL / 32) + (threadIdx.x >> 5) : blockIdx.x;
+    Sum<2, BY, BY == BY_CLUSTER> sum = sum_of<2, BY, BY == BY_CLUSTER>(P, box, &ex);
+    const Place<BY, V, E> at(P);
+    int64_t r = at.row;
     const T *__restrict__ dy = static_cast<const T *>(P.dy);
-    const int width = P.width;
-    float w[HOLD ? NV : 1][V], dw[NV][V], db[NV][V];
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        if constexpr (HOLD) load_vector<V>(w[i], P.w, P.w_type, (i * span + tid) * V, width, 1.f);
-#pragma unroll
-        for (int j = 0; j < V; ++j) dw[i][j] = db[i][j] = 0.f;
-    }
-    Source<S, V> nx[NV];
-    Piece<T, V> ndy[NV];
+    constexpr bool PACKED = std::is_same<S, Packed8>::value;
+    constexpr int ONE = V == 1 ? E : 1;
+    HeldSource<S, ONE> nx;                 // (V = 1)
+    Held<T, 1, ONE> ndy;
+    Ring<STAGES> ring;                     // (V = 8)
+    const unsigned columns = (unsigned)max(0, min(P.width - at.col0, P.group * E)), held = P.group * E;
+    const unsigned x_bytes = PACKED ? (columns + 15) & ~15u : columns * SOURCE_BYTES<S>, dy_bytes = columns * (unsigned)sizeof(T);
     float nmean = 0.f, nrstd = 0.f;
-    auto fetch = [&](int64_t row) {
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int c = (i * span + tid) * V;
-            nx[i].zero();
-            ndy[i].zero();
-            if (row < P.n_rows && c < width) {
-                nx[i].load(P, row, c);
-                ndy[i].load(dy + row * P.dys + c);
-            }
-        }
-        if (row < P.n_rows) { nmean = P.mean[row]; nrstd = P.rstd[row]; }
+    unsigned nscale[E / 8];                // (packed, V = 8)
+    auto issue = [&](int i, int64_t row) {
+        ring.expect(i, x_bytes + dy_bytes);
+        if constexpr (PACKED) ring.copy(i, 0, P.q + row * P.qs + at.col0, x_bytes);
+        else ring.copy(i, 0, static_cast<const S *>(P.x) + row * P.xs + at.col0, x_bytes);
+        ring.copy(i, held * SOURCE_BYTES<S>, dy + row * P.dys + at.col0, dy_bytes);
     };
-    fetch(r);
-    for (; r < P.n_rows; r += step) {
-        float xh[NV][V], d[NV][V];
-        const float mean = nmean, rstd = nrstd;
-        float2 s = make_float2(0.f, 0.f);
+    // what is a few bytes a thread, one row ahead
+    auto fetch = [&](int64_t row) {
+        if (row >= P.n_rows) return;
+        nmean = P.mean[row];
+        nrstd = P.rstd[row];
+        if constexpr (V == 1) {
+            nx.fetch(P, row, at.col, at.rem);
+            ndy.fetch(dy + row * P.dys + at.col, at.rem);
+        } else if constexpr (PACKED) {
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int c = (i * span + tid) * V;
-            nx[i].get(xh[i]);
-            ndy[i].get(d[i]);
-            float wr[V];
-            if constexpr (!HOLD) load_vector<V>(wr, P.w, P.w_type, c, width, 1.f);
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-                xh[i][j] = (xh[i][j] - mean) * rstd;
-                if (c >= width) xh[i][j] = 0.f;            // (an infinite rstd or a NaN mean must not reach the sums from behind the row)
-                dw[i][j] += d[i][j] * xh[i][j];
-                db[i][j] += d[i][j];
-                d[i][j] *= HOLD ? w[HOLD ? i : 0][j] : wr[j];
-                s.x += d[i][j];
-                s.y += d[i][j] * xh[i][j];
-            }
+            for (int i = 0; i < E / 8; ++i) if (Of<8>::place(i) < at.rem) nscale[i] = P.scale[row * P.ss + (at.col + Of<8>::place(i)) / TAD_BLOCK8];
         }
-        fetch(r + step);
-        s = sum.template of<WARP>(s);
-        const float c1 = s.x * P.inv_width, c2 = s.y * P.inv_width;
-        if (P.dx) {
+    };
+    if constexpr (V == 8) {
+        const unsigned stage = held * (SOURCE_BYTES<S> + (unsigned)sizeof(T));
+        ring.start(rows, at.group * STAGES * stage, smem_u32(&bars[at.group][0]), stage, at.in == 0);
+        clear_ring(rows, blockDim.x * STAGES * E * (SOURCE_BYTES<S> + (unsigned)sizeof(T)));
+        __syncthreads();
+        if (ring.leader)
+            for (int i = 0; i < STAGES; ++i) if (r + i * at.step < P.n_rows) issue(i, r + i * at.step);
 #pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                const int c = (i * span + tid) * V;
-                if (c >= width) continue;
-                float o[V];
+        for (int i = 0; i < E / 8; ++i) nscale[i] = 127;
+    } else {
+        nx.zero();
+        ndy.zero();
+    }
+    fetch(r);
+    Pairs<E> w, dws, dbs;
+    {
+        float f[E];
+        load_vector<V, E>(f, P.w, P.w_type, at.col, at.rem, 1.f);
+        w.set(f);
+    }
 #pragma unroll
-                for (int j = 0; j < V; ++j) o[j] = rstd * (d[i][j] - c1 - xh[i][j] * c2);
-                store_typed<V>(P.dx, P.dx_type, r * P.dxs + c, o);
+    for (int j = 0; j < E / 2; ++j) dws.p[j] = dbs.p[j] = make_float2(0.f, 0.f);
+    for (; r < P.n_rows; r += at.step) {
+        float xh[E], d[E];
+        const float mean = nmean;
+        float rstd = nrstd;
+        if constexpr (V == 8) {
+            const unsigned char *from = ring.row();
+            const int c = at.col - at.col0;
+            ring.wait();
+            if constexpr (PACKED) {
+#pragma unroll
+                for (int i = 0; i < E / 8; ++i) {
+                    uint2 q = *reinterpret_cast<const uint2 *>(from + c + Of<8>::place(i));
+                    if (Of<8>::place(i) >= at.rem) q = make_uint2(0, 0);     // (copies end on whole sixteens, eight bytes behind the row at most)
+                    float f[8];
+                    unpack_eight(q, scale_of(nscale[i]), f);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) xh[i * 8 + j] = f[j];
+                }
+            } else {
+                Piece<S, 8> p[E / 8];
+                read_row<S, E>(p, reinterpret_cast<const S *>(from) + c);
+                elements<S, E>(xh, p);
             }
+            Piece<T, 8> p[E / 8];
+            read_row<T, E>(p, reinterpret_cast<const T *>(from + held * SOURCE_BYTES<S>) + c);
+            elements<T, E>(d, p);
+        } else {
+            nx.get(xh);
+            ndy.get(d);
+        }
+        fetch(r + at.step);
+        if (V == 8 && ring.lost) rstd = __uint_as_float(0x7fffffffu);        // (a row that never came has no result)
+        Pairs<E> h, g;
+        h.set(xh);
+        g.set(d);
+        float2 s1 = make_float2(0.f, 0.f), s2 = s1;
+#pragma unroll
+        for (int j = 0; j < E / 2; ++j) {
+            // behind the row xh is zero: zero times an infinite rstd or a NaN mean would reach the sums
+            h.p[j] = __fmul2_rn(__fadd2_rn(h.p[j], inside<V>(-mean, j, at.rem)), inside<V>(rstd, j, at.rem));
+            dws.p[j] = __ffma2_rn(g.p[j], h.p[j], dws.p[j]);
+            dbs.p[j] = __fadd2_rn(dbs.p[j], g.p[j]);
+            g.p[j] = __fmul2_rn(g.p[j], w.p[j]);
+            s1 = __fadd2_rn(s1, g.p[j]);
+            s2 = __ffma2_rn(g.p[j], h.p[j], s2);
+        }
+        float s[2] = {s1.x + s1.y, s2.x + s2.y};
+        sum.of(s);
+        if constexpr (V == 8) {
+            // (behind the sum every thread of the group has read the row)
+            if (ring.leader && !ring.lost && r + STAGES * at.step < P.n_rows) issue(ring.at, r + STAGES * at.step);
+            ring.advance();
+        }
+        if (P.dx) {
+            const float c1 = -s[0] * P.inv_width, c2 = -s[1] * P.inv_width;
+            const float2 rr = make_float2(rstd, rstd), m1 = make_float2(c1, c1), m2 = make_float2(c2, c2);
+#pragma unroll
+            for (int j = 0; j < E / 2; ++j) g.p[j] = __fmul2_rn(rr, __ffma2_rn(h.p[j], m2, __fadd2_rn(g.p[j], m1)));
+            g.get(d);
+            store_typed<V, E>(P.dx, P.dx_type, r * P.dxs + at.col, at.rem, d);
         }
     }
+    sum.finish();
     if (!P.planes) return;
-    float *plane = P.planes + (size_t)blockIdx.x * 2 * width;
-    if constexpr (WARP) {
+    float dw[E], db[E];
+    dws.get(dw);
+    dbs.get(db);
+    if constexpr (BY == BY_CLUSTER) {
+        // one group a block: it owns its columns in the plane of its cluster
+        float *plane = P.planes + (size_t)at.row * 2 * P.width + at.col;
 #pragma unroll
-        for (int k = 0; k < 2; ++k)
-#pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                __syncthreads();
-#pragma unroll
-                for (int j = 0; j < V; ++j) join[threadIdx.x >> 5][tid * V + j] = k ? db[i][j] : dw[i][j];
-                __syncthreads();
-                for (int e = threadIdx.x; e < 32 * V; e += SMALL) {
-                    const int c = i * 32 * V + e;
-                    float a = 0.f;
-#pragma unroll
-                    for (int q = 0; q < SMALL / 32; ++q) a += join[q][e];
-                    if (c < width) plane[(size_t)k * width + c] = a;
-                }
+        for (int e = 0; e < E; ++e)
+            if (Of<V>::place(e / V) < at.rem) {
+                plane[Of<V>::column(e)] = dw[e];
+                plane[(size_t)P.width + Of<V>::column(e)] = db[e];
             }
     } else {
+        // the groups of the block are added up in order, eight elements of every thread at a time
+        float *plane = P.planes + (size_t)blockIdx.x * 2 * P.width;
+        const int groups = blockDim.x / P.group;
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
+        for (int part = 0; part < E / 4; ++part) {
+            __syncthreads();
 #pragma unroll
-            for (int j = 0; j < V; ++j) {
-                const int c = (i * span + tid) * V + j;
-                if (c < width) { plane[c] = dw[i][j]; plane[(size_t)width + c] = db[i][j]; }
+            for (int k = 0; k < 8; ++k) join[threadIdx.x][k] = part < E / 8 ? dw[part % (E / 8) * 8 + k] : db[part % (E / 8) * 8 + k];
+            __syncthreads();
+            for (int u = threadIdx.x; u < P.group * 8; u += blockDim.x) {
+                const int t = u >> 3, e = part % (E / 8) * 8 + (u & 7);
+                const int c = (t >> 5) * (32 * E) + (t & 31) * V + Of<V>::column(e);
+                float a = 0.f;
+                for (int g = 0; g < groups; ++g) a += join[g * P.group + t][u & 7];
+                if (c < P.width) plane[(part < E / 8 ? 0 : (size_t)P.width) + c] = a;
             }
+        }
     }
 }
 
@@ -340,9 +758,9 @@ template <class S, class T>
 __global__ void __launch_bounds__(LARGE)
 tad_norm_backward_long_kernel(const Params P)
 {
-    __shared__ float2 box[2][32];
+    __shared__ float box[2][2][32];
     tad_wait_previous();
-    Sum sum{box, 0};
+    int turn = 0;
     const T *__restrict__ dys = static_cast<const T *>(P.dy);
     for (int64_t r = blockIdx.x; r < P.n_rows; r += gridDim.x) {
         const T *dy = dys + r * P.dys;
@@ -363,7 +781,13 @@ tad_norm_backward_long_kernel(const Params P)
             s.x += g;
             s.y += g * xh;
         }
-        s = sum.of<false>(s);
+        s.x = warp_sum(s.x);
+        s.y = warp_sum(s.y);
+        if ((threadIdx.x & 31) == 0) { box[turn][0][threadIdx.x >> 5] = s.x; box[turn][1][threadIdx.x >> 5] = s.y; }
+        __syncthreads();
+        s.x = warp_sum(box[turn][0][threadIdx.x & 31]);
+        s.y = warp_sum(box[turn][1][threadIdx.x & 31]);
+        turn ^= 1;
         const float c1 = s.x * P.inv_width, c2 = s.y * P.inv_width;
 #pragma unroll 4
         for (int c = threadIdx.x; c < P.width; c += LARGE) {
@@ -425,55 +849,80 @@ tad_norm_planes_kernel(const float *__restrict__ planes, int n_planes, int width
 
 // ---- host ----
 
-struct Shape { int threads; int64_t most; bool warp, hold, is_long; };          // most: blocks that a B200 runs at a time
-Shape shape_of(int64_t width, int sm_threads)
+// rows of `width` columns by blocks of at most `block` threads, `e` elements a thread
+struct Shape { int by, group, cluster; };
+Shape shape_of(int64_t width, int block, int e)
 {
     Shape s{};
-    s.warp = width <= WARP_WIDTH;
-    s.is_long = width > HELD;
-    s.threads = s.warp ? SMALL : s.is_long ? LARGE : (int)((width + 32 * E - 1) / (32 * E)) * 32;
-    s.hold = s.threads <= SMALL;
-    s.most = (int64_t)SMS * std::max(1, std::min(32, sm_threads / s.threads));
+    s.cluster = 1;
+    while (s.cluster * (int64_t)block * e < width && s.cluster < MAX_CLUSTER) s.cluster *= 2;
+    const int warps = (int)((width + 32 * e - 1) / (32 * e));
+    s.by = s.cluster > 1 ? BY_CLUSTER : warps > 1 ? BY_GROUP : BY_WARP;
+    s.group = s.by == BY_CLUSTER ? block : s.by == BY_WARP ? 32 : (warps + 1) / 2 * 64;      // (warps in pairs: their sums are read in pairs)
     return s;
 }
-constexpr int FORWARD_THREADS = 768, BACKWARD_THREADS = 512;        // of an SM that the registers of the kernels allow
 
-// planes of partial sums of the backward pass: one a block
-int64_t planes_of(int64_t n_rows, int64_t width)
+// Planes of partial sums of the backward pass, one a block or cluster: one block an SM, as many groups in it as fit.  The workspace has
+// room for those of either number of elements a thread.
+int64_t planes_of(int64_t n_rows, int64_t width, int e)
 {
-    const Shape s = shape_of(width, BACKWARD_THREADS);
-    if (s.is_long) return std::max<int64_t>(1, std::min<int64_t>(n_rows, 64));
-    const int64_t blocks = s.warp ? (n_rows + SMALL / 32 - 1) / (SMALL / 32) : n_rows;
-    return std::max<int64_t>(1, std::min(blocks, s.most));
+    if (width > HELD) return std::max<int64_t>(1, std::min<int64_t>(n_rows, 64));
+    const Shape s = shape_of(width, BACKWARD_BLOCK, e);
+    const int groups = s.by == BY_CLUSTER ? 1 : BACKWARD_BLOCK / s.group;
+    return std::max<int64_t>(1, std::min<int64_t>((n_rows + groups - 1) / groups, SMS / s.cluster));
 }
 
 template <class T>
 cudaError_t forward(const Params &P, const Shape &s, bool eights, bool keep, cudaStream_t stream)
 {
-    if (s.is_long) return tad_launch(tad_norm_forward_long_kernel<T>, (unsigned)std::min<int64_t>(P.n_rows, 2 * SMS), LARGE, 0, stream, P);
-    const int64_t want = s.warp ? (P.n_rows + SMALL / 32 - 1) / (SMALL / 32) : P.n_rows;
-    const unsigned blocks = (unsigned)std::min(want, s.most);
-    auto kernel = tad_norm_forward_kernel<T, 1, true, true, false>;
-    if (eights && keep) kernel = s.warp ? tad_norm_forward_kernel<T, 8, true, true, true> : s.hold ? tad_norm_forward_kernel<T, 8, false, true, true> : tad_norm_forward_kernel<T, 8, false, false, true>;
-    else if (eights) kernel = s.warp ? tad_norm_forward_kernel<T, 8, true, true, false> : s.hold ? tad_norm_forward_kernel<T, 8, false, true, false> : tad_norm_forward_kernel<T, 8, false, false, false>;
-    else if (!s.warp) kernel = s.hold ? tad_norm_forward_kernel<T, 1, false, true, false> : tad_norm_forward_kernel<T, 1, false, false, false>;
-    return tad_launch(kernel, blocks, s.threads, 0, stream, P);
+    if (P.width > HELD) return tad_launch(tad_norm_forward_long_kernel<T>, (unsigned)std::min<int64_t>(P.n_rows, 2 * SMS), LARGE, 0, stream, P);
+    const int threads = s.by == BY_WARP ? FORWARD_BLOCK : s.group, groups = s.by == BY_WARP ? FORWARD_BLOCK / 32 : 1;
+    const int64_t most = (int64_t)SMS * std::min(32, (eights ? FORWARD_BLOCKS : 2) * FORWARD_BLOCK / threads) / s.cluster;
+    const unsigned blocks = (unsigned)(std::min((P.n_rows + groups - 1) / groups, most) * s.cluster);
+    auto kernel = tad_norm_forward_kernel<T, 1, BY_WARP, false>;
+    constexpr int VK = sizeof(T) == 2 ? 16 : 8;
+    if (eights && keep) kernel = s.by == BY_WARP ? tad_norm_forward_kernel<T, VK, BY_WARP, true> : s.by == BY_GROUP ? tad_norm_forward_kernel<T, VK, BY_GROUP, true> : tad_norm_forward_kernel<T, VK, BY_CLUSTER, true>;
+    else if (eights) kernel = s.by == BY_WARP ? tad_norm_forward_kernel<T, 8, BY_WARP, false> : s.by == BY_GROUP ? tad_norm_forward_kernel<T, 8, BY_GROUP, false> : tad_norm_forward_kernel<T, 8, BY_CLUSTER, false>;
+    else if (s.by != BY_WARP) kernel = s.by == BY_GROUP ? tad_norm_forward_kernel<T, 1, BY_GROUP, false> : tad_norm_forward_kernel<T, 1, BY_CLUSTER, false>;
+    const size_t smem = eights ? (size_t)threads * FORWARD_E * sizeof(T) * FORWARD_STAGES<T> : 0;      // (32 KB at most)
+    return tad_launch_cluster(kernel, blocks, threads, smem, stream, s.cluster, P);
 }
 
+// also says how many planes there are
 template <class S, class T>
-cudaError_t backward(const Params &P, const Shape &s, bool eights, int64_t planes, cudaStream_t stream)
+cudaError_t backward(Params &P, bool eights, int64_t &planes, cudaStream_t stream)
 {
-    if (s.is_long) {
+    const int e8 = eights ? BACKWARD_E<8> : BACKWARD_E<1>;
+    planes = planes_of(P.n_rows, P.width, e8);
+    const Shape s = shape_of(P.width, BACKWARD_BLOCK, e8);
+    P.group = s.group;
+    if (P.width > HELD) {
         cudaError_t e = cudaSuccess;
         if (P.dx) e = tad_launch(tad_norm_backward_long_kernel<S, T>, (unsigned)std::min<int64_t>(P.n_rows, 2 * SMS), LARGE, 0, stream, P);
         if (e == cudaSuccess && P.planes)
             e = tad_launch(tad_norm_columns_kernel<S, T>, dim3((unsigned)((P.width + SMALL - 1) / SMALL), (unsigned)planes), SMALL, 0, stream, P, (P.n_rows + planes - 1) / planes);
         return e;
     }
-    auto kernel = tad_norm_backward_kernel<S, T, 1, true, true>;
-    if (eights) kernel = s.warp ? tad_norm_backward_kernel<S, T, 8, true, true> : s.hold ? tad_norm_backward_kernel<S, T, 8, false, true> : tad_norm_backward_kernel<S, T, 8, false, false>;
-    else if (!s.warp) kernel = s.hold ? tad_norm_backward_kernel<S, T, 1, false, true> : tad_norm_backward_kernel<S, T, 1, false, false>;
-    return tad_launch(kernel, (unsigned)planes, s.threads, 0, stream, P);
+    auto kernel = tad_norm_backward_kernel<S, T, 1, BY_WARP>;
+    if (eights) kernel = s.by == BY_WARP ? tad_norm_backward_kernel<S, T, 8, BY_WARP> : s.by == BY_GROUP ? tad_norm_backward_kernel<S, T, 8, BY_GROUP> : tad_norm_backward_kernel<S, T, 8, BY_CLUSTER>;
+    else if (s.by != BY_WARP) kernel = s.by == BY_GROUP ? tad_norm_backward_kernel<S, T, 1, BY_GROUP> : tad_norm_backward_kernel<S, T, 1, BY_CLUSTER>;
+    const int threads = s.by == BY_CLUSTER ? s.group : BACKWARD_BLOCK / s.group * s.group;
+    size_t smem = 0;
+    if (eights) {
+        constexpr size_t most = (size_t)BACKWARD_BLOCK * BACKWARD_E<8> * (SOURCE_BYTES<S> + sizeof(T)) * BACKWARD_STAGES<S, T>;
+        static_assert(most <= 163840, "rows ahead and the join of the groups fit into shared memory");
+        static std::atomic<bool> allowed[64][3];
+        int dev = -1;
+        cudaError_t e = cudaGetDevice(&dev);
+        if (e != cudaSuccess) return e;
+        if (dev < 0 || dev >= 64 || !allowed[dev][s.by].load(std::memory_order_relaxed)) {
+            e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most);
+            if (e != cudaSuccess) return e;
+            if (dev >= 0 && dev < 64) allowed[dev][s.by].store(true, std::memory_order_relaxed);
+        }
+        smem = (size_t)threads * BACKWARD_E<8> * (SOURCE_BYTES<S> + sizeof(T)) * BACKWARD_STAGES<S, T>;
+    }
+    return tad_launch_cluster(kernel, (unsigned)(planes * s.cluster), threads, smem, stream, s.cluster, P);
 }
 
 }  // namespace
@@ -504,8 +953,9 @@ tad_status tad_layernorm_forward(const tad_rows *x, int64_t n_rows, int64_t widt
     if (bias) { P.b = bias->data; P.b_type = bias->type; }
     P.mean = mean; P.rstd = rstd;
     P.n_rows = n_rows; P.width = (int)width; P.eps = eps; P.inv_width = 1.f / (float)width;
-    const Shape s = shape_of(width, FORWARD_THREADS);
-    const bool eights = width % 8 == 0 && by_eights(x) && by_eights(y), keep = checkpoint && eights && !s.is_long;
+    const Shape s = shape_of(width, FORWARD_BLOCK, FORWARD_E);
+    P.group = s.group;
+    const bool eights = width % 8 == 0 && by_eights(x) && by_eights(y), keep = checkpoint && eights && width <= HELD;
     if (keep) { P.kq = checkpoint->q; P.kqs = checkpoint->q_stride; P.kscale = checkpoint->scale; P.kss = checkpoint->scale_stride; }
     else if (checkpoint && (st = tad_launch_pack8(x, n_rows, width, checkpoint, stream))) return st;
     cudaError_t e = cudaSuccess;
@@ -516,7 +966,7 @@ tad_status tad_layernorm_forward(const tad_rows *x, int64_t n_rows, int64_t widt
 size_t tad_layernorm_workspace_bytes(int64_t n_rows, int64_t width)
 {
     if (n_rows <= 0 || width <= 0 || n_rows >= MAX_ROWS || width >= MAX_WIDTH) return 0;
-    return ((size_t)planes_of(n_rows, width) * 2 * (size_t)width * 4 + 255) & ~size_t(255);
+    return ((size_t)std::max(planes_of(n_rows, width, 16), planes_of(n_rows, width, 8)) * 2 * (size_t)width * 4 + 255) & ~size_t(255);
 }
 
 tad_status tad_layernorm_backward(const tad_rows *dy, const tad_rows *x, const tad_packed *checkpoint, int64_t n_rows, int64_t width,
@@ -551,12 +1001,10 @@ tad_status tad_layernorm_backward(const tad_rows *dy, const tad_rows *x, const t
         P.mean = const_cast<float *>(mean); P.rstd = const_cast<float *>(rstd);
         P.planes = sums ? static_cast<float *>(workspace) : nullptr;
         P.n_rows = n_rows; P.width = (int)width; P.inv_width = 1.f / (float)width;
-        const Shape s = shape_of(width, BACKWARD_THREADS);
-        const bool eights = width % 8 == 0 && by_eights(dy) && (!x || by_eights(x)) && (!dx || by_eights(dx));
-        planes = planes_of(n_rows, width);
+                const bool eights = width % 8 == 0 && by_eights(dy) && (!x || by_eights(x)) && (!dx || by_eights(dx));
         TAD_WITH_TYPE(dy->type, T, {
-            if (!x) e = backward<Packed8, T>(P, s, eights, planes, stream);
-            else TAD_WITH_TYPE(x->type, S, e = backward<S, T>(P, s, eights, planes, stream));
+            if (!x) e = backward<Packed8, T>(P, eights, planes, stream);
+            else TAD_WITH_TYPE(x->type, S, e = (backward<S, T>(P, eights, planes, stream)));
         });
     }
     if (e == cudaSuccess && sums)

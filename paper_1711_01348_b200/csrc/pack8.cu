@@ -13,163 +13,259 @@ using namespace tadr;
 
 constexpr int NT = 256, ROWS = 4;          // threads of a block; rows that a thread has under way
 
-// Sixteen threads own a block of 128, eight elements each.  A thread block covers CB = 2^cb_log blocks of a row (16 or, in narrow
-// matrices, the whole row) and ROWS x 16 / CB rows.
+// A block of 128 belongs to 2^own neighbouring threads: to pack, eight (sixteen elements each); to unpack, sixteen, because a thread's store
+// is one piece of 16 bytes then (two of them, 32 bytes apart in a warp: 81 % of the memory rate for 97 %); off 16-byte boundaries a
+// warp, whose lanes take every 32nd element.  A thread block covers 2^cb blocks of a row (all that its threads own or, in narrow
+// matrices, the whole row), and ROWS times as many rows as that leaves it threads for.
 struct Cover {
     int64_t row0;            // first row of this thread, the next ones are `step` rows on
-    int step, blk;           // its block of 128 in the row
-    int col;                 // first of its eight elements
-    __device__ __forceinline__ Cover(int cb_log, unsigned chunks)
+    int step, blk, in;       // its block of 128 in the row, its place among the block's threads
+    __device__ __forceinline__ Cover(int own, int cb, unsigned chunks)
     {
         const unsigned group = blockIdx.x / chunks, chunk = blockIdx.x - group * chunks;
-        const int b = threadIdx.x >> 4;
-        step = 16 >> cb_log;
-        row0 = (int64_t)group * (ROWS * step) + (b >> cb_log);
-        blk = (int)(chunk << cb_log) + (b & ((1 << cb_log) - 1));
-        col = blk * TAD_BLOCK8 + (threadIdx.x & 15) * 8;
+        const int b = threadIdx.x >> own;
+        step = (NT >> own) >> cb;
+        row0 = (int64_t)group * (ROWS * step) + (b >> cb);
+        blk = (int)(chunk << cb) + (b & ((1 << cb) - 1));
+        in = threadIdx.x & ((1 << own) - 1);
     }
 };
+constexpr int OWN_PACK = 3, OWN_UNPACK = 4, OWN_ODD = 5;
 
-// eight elements from c on, zeros behind the row; VEC: 16-byte loads where all eight exist
-template <class T, bool VEC>
-__device__ __forceinline__ void load_eight(float (&v)[8], const T *__restrict__ row, int c, int width)
-{
-    if (VEC && c + 8 <= width) {
-        Piece<T, 8> p;
-        p.load(row + c);
-        p.get(v);
-    } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = c + j < width ? to_float(row[c + j]) : 0.f;
-    }
-}
-
-__device__ __forceinline__ float max_of_block(float a)
-{
-#pragma unroll
-    for (int d = 8; d; d >>= 1) a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, d));
-    return a;
-}
-
-template <class T, bool VEC>
+template <class T>
 __global__ void __launch_bounds__(NT)
-tad_pack8_kernel(const T *__restrict__ x, int64_t xs, int64_t n_rows, int width, int n_blocks, int cb_log, unsigned chunks,
+tad_pack8_kernel(const T *__restrict__ x, int64_t xs, int64_t n_rows, int width, int cb, unsigned chunks,
                  uint8_t *__restrict__ q, int64_t qs, uint8_t *__restrict__ scale, int64_t ss)
 {
     tad_wait_previous();
-    const Cover at(cb_log, chunks);
-    float v[ROWS][8];
+    const Cover at(OWN_PACK, cb, chunks);
+    const int col = at.blk * TAD_BLOCK8 + at.in * 16;
+    Sixteen<T> v[ROWS];
 #pragma unroll
     for (int i = 0; i < ROWS; ++i) {
         const int64_t r = at.row0 + i * at.step;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[i][j] = 0.f;
-        if (r < n_rows && at.col < width) load_eight<T, VEC>(v[i], x + r * xs, at.col, width);
+        v[i].zero();
+        if (r < n_rows && col < width) v[i].load(x + r * xs, col, width);
     }
 #pragma unroll
     for (int i = 0; i < ROWS; ++i) {
         const int64_t r = at.row0 + i * at.step;
-        float a = 0.f;
+        unsigned s;
+        const uint4 u = v[i].pack(s);
+        if (r >= n_rows || col >= width) continue;
+        uint8_t *to = q + r * qs + col;
+        if (col + 16 <= width) *reinterpret_cast<uint4 *>(to) = u;
+        else {
+            const unsigned words[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
-        for (int j = 0; j < 8; ++j) a = fmaxf(a, finite_abs(v[i][j]));
-        const unsigned s = scale_byte(max_of_block(a));
-        if (r >= n_rows || at.col >= width) continue;
-        const uint2 p = pack_eight(v[i], inverse_scale(s));
-        uint8_t *to = q + r * qs + at.col;
-        if (at.col + 8 <= width) *reinterpret_cast<uint2 *>(to) = p;
-        else for (int j = 0; j < width - at.col; ++j) to[j] = (uint8_t)((j < 4 ? p.x : p.y) >> (8 * (j & 3)));
-        if ((threadIdx.x & 15) == 0) scale[r * ss + at.blk] = (uint8_t)s;
+            for (int j = 0; j < 16; ++j) if (col + j < width) to[j] = (uint8_t)(words[j >> 2] >> (8 * (j & 3)));
+        }
+        if (at.in == 0) scale[r * ss + at.blk] = (uint8_t)s;
     }
 }
 
-template <class T, bool VEC>
+template <class T>
 __global__ void __launch_bounds__(NT)
 tad_unpack8_kernel(const uint8_t *__restrict__ q, int64_t qs, const uint8_t *__restrict__ scale, int64_t ss, int64_t n_rows, int width,
-                   int cb_log, unsigned chunks, T *__restrict__ x, int64_t xs)
+                   int cb, unsigned chunks, T *__restrict__ x, int64_t xs)
 {
     tad_wait_previous();
-    const Cover at(cb_log, chunks);
+    const Cover at(OWN_UNPACK, cb, chunks);
+    const int col = at.blk * TAD_BLOCK8 + at.in * 8;
     uint2 p[ROWS];
     unsigned s[ROWS];
 #pragma unroll
     for (int i = 0; i < ROWS; ++i) {
         const int64_t r = at.row0 + i * at.step;
-        if (r < n_rows && at.col < width) {
+        if (r < n_rows && col < width) {
             // (rows of q are a multiple of 16 long: all eight bytes exist)
-            p[i] = *reinterpret_cast<const uint2 *>(q + r * qs + at.col);
+            p[i] = *reinterpret_cast<const uint2 *>(q + r * qs + col);
             s[i] = scale[r * ss + at.blk];
         }
     }
 #pragma unroll
     for (int i = 0; i < ROWS; ++i) {
         const int64_t r = at.row0 + i * at.step;
-        if (r >= n_rows || at.col >= width) continue;
+        if (r >= n_rows || col >= width) continue;
         float v[8];
         unpack_eight(p[i], scale_of(s[i]), v);
-        T *to = x + r * xs + at.col;
-        if (VEC && at.col + 8 <= width) {
+        T *to = x + r * xs + col;
+        if (col + 8 <= width) {
             Piece<T, 8> o;
             o.set(v);
             o.store(to);
         } else {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) if (at.col + j < width) to[j] = from_float<T>(v[j]);
+            for (int j = 0; j < 8; ++j) if (col + j < width) to[j] = from_float<T>(v[j]);
         }
     }
 }
 
-// The transpose, 128 x 128 elements a thread block: warp w holds rows 16 w .. 16 w + 15 and lane g columns 4 g .. 4 g + 3 in
-// registers (a row is one coalesced line of 128 bytes), the largest value of a column is found over the warps through shared
-// memory, and the packed columns pass through shared memory as 16-byte units, unit u of column c at place u ^ ((c / 4) mod 8), so that
-// neither side has bank conflicts and each row of the output gets its 128 bytes at once.
+// rows of x off 16-byte boundaries
+template <class T>
 __global__ void __launch_bounds__(NT)
+tad_pack8_odd_kernel(const T *__restrict__ x, int64_t xs, int64_t n_rows, int width, int cb, unsigned chunks,
+                     uint8_t *__restrict__ q, int64_t qs, uint8_t *__restrict__ scale, int64_t ss)
+{
+    tad_wait_previous();
+    const Cover at(OWN_ODD, cb, chunks);
+    const int col = at.blk * TAD_BLOCK8 + at.in;
+    T raw[ROWS][4];
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+        const int64_t r = at.row0 + i * at.step;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            raw[i][j] = from_float<T>(0.f);
+            if (r < n_rows && col + 32 * j < width) raw[i][j] = x[r * xs + col + 32 * j];
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+        const int64_t r = at.row0 + i * at.step;
+        float v[4], a = 0.f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) { v[j] = to_float(raw[i][j]); a = fmaxf(a, finite_abs(v[j])); }
+#pragma unroll
+        for (int d = 16; d; d >>= 1) a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, d));
+        if (r >= n_rows) continue;
+        const unsigned s = scale_byte(a);
+        const float inv = inverse_scale(s);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) if (col + 32 * j < width) q[r * qs + col + 32 * j] = (uint8_t)to_e4m3x2(no_infinity(v[j]) * inv, 0.f);
+        if (at.in == 0 && col < width) scale[r * ss + at.blk] = (uint8_t)s;
+    }
+}
+
+template <class T>
+__global__ void __launch_bounds__(NT)
+tad_unpack8_odd_kernel(const uint8_t *__restrict__ q, int64_t qs, const uint8_t *__restrict__ scale, int64_t ss, int64_t n_rows, int width,
+                       int cb, unsigned chunks, T *__restrict__ x, int64_t xs)
+{
+    tad_wait_previous();
+    const Cover at(OWN_ODD, cb, chunks);
+    const int col = at.blk * TAD_BLOCK8 + at.in;
+    uint8_t p[ROWS][4];
+    unsigned s[ROWS];
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+        const int64_t r = at.row0 + i * at.step;
+        s[i] = 127;
+        if (r < n_rows && col < width) s[i] = scale[r * ss + at.blk];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            p[i][j] = 0;
+            if (r < n_rows && col + 32 * j < width) p[i][j] = q[r * qs + col + 32 * j];
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+        const int64_t r = at.row0 + i * at.step;
+        const float f = scale_of(s[i]);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) if (r < n_rows && col + 32 * j < width) x[r * xs + col + 32 * j] = from_float<T>(from_e4m3x2(p[i][j]).x * f);
+    }
+}
+
+// The transpose, 128 x 128 elements a thread block: warp w holds rows 16 w .. 16 w + 15 and lane g columns 4 g .. 4 g + 3 in
+// registers (a row is one coalesced line of 128 bytes), turned at once into words of four rows of a column.  The largest value of a
+// column is found over the warps through shared memory, and the packed columns pass through shared memory as 16-byte units,
+// unit u of column c at place u ^ ((c / 4) mod 8), so that neither side has bank conflicts and each row of the output gets its 128
+// bytes at once.  Values are formed twice from the bytes: kept, they take 64 registers more.
+__global__ void __launch_bounds__(NT, 3)
 tad_repack8_kernel(const uint8_t *__restrict__ q, int64_t qs, const uint8_t *__restrict__ scale, int64_t ss, int64_t n_rows, int width,
                    unsigned tiles_c, uint8_t *__restrict__ out, int64_t os, uint8_t *__restrict__ oscale, int64_t oss)
 {
-    __shared__ float most[8][128];
+    __shared__ __align__(16) float most[8][128], row_scale[128];
     __shared__ uint4 tile[128 * 8];
     tad_wait_previous();
     const unsigned tr = blockIdx.x / tiles_c, tc = blockIdx.x - tr * tiles_c;
     const int warp = threadIdx.x >> 5, g = threadIdx.x & 31;
     const int64_t r0 = (int64_t)tr * 128;
     const int c0 = (int)tc * 128, c = c0 + 4 * g;
-    unsigned w[16], s[16];
+    if (threadIdx.x < 128) row_scale[threadIdx.x] = r0 + threadIdx.x < n_rows ? scale_or_infinity(scale[(r0 + threadIdx.x) * ss + tc]) : 1.f;
+    unsigned t[4][4];                      // [column][four rows]
+    {
+        unsigned w[16];
+        const uint8_t *from = q + (r0 + warp * 16) * qs + c;
+        const int rows = c < width ? (int)min((int64_t)16, n_rows - r0 - warp * 16) : 0;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        const int64_t r = r0 + warp * 16 + i;
-        const bool live = r < n_rows && c < width;
-        w[i] = live ? *reinterpret_cast<const unsigned *>(q + r * qs + c) : 0u;
-        s[i] = live ? scale[r * ss + tc] : 127u;
+        for (int i = 0; i < 16; ++i) {
+            w[i] = 0;
+            if (i < rows) w[i] = *reinterpret_cast<const unsigned *>(from);
+            from += qs;
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const unsigned lo0 = __byte_perm(w[4 * k], w[4 * k + 1], 0x5140), hi0 = __byte_perm(w[4 * k], w[4 * k + 1], 0x7362);
+            const unsigned lo1 = __byte_perm(w[4 * k + 2], w[4 * k + 3], 0x5140), hi1 = __byte_perm(w[4 * k + 2], w[4 * k + 3], 0x7362);
+            t[0][k] = __byte_perm(lo0, lo1, 0x5410); t[1][k] = __byte_perm(lo0, lo1, 0x7632);
+            t[2][k] = __byte_perm(hi0, hi1, 0x5410); t[3][k] = __byte_perm(hi0, hi1, 0x7632);
+        }
     }
-    float v[16][4], a[4] = {0.f, 0.f, 0.f, 0.f};
+    __syncthreads();
+    // rows 4 k .. 4 k + 3 of a column, with their scales
+    auto values = [&](unsigned word, const float4 &f, float2 &x, float2 &y) {
+        x = __fmul2_rn(from_e4m3x2(word & 0xffffu), make_float2(f.x, f.y));
+        y = __fmul2_rn(from_e4m3x2(word >> 16), make_float2(f.z, f.w));
+    };
+    float a[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        const float f = scale_of(s[i]);
-        const float2 lo = from_e4m3x2(w[i] & 0xffffu), hi = from_e4m3x2(w[i] >> 16);
-        v[i][0] = lo.x * f; v[i][1] = lo.y * f; v[i][2] = hi.x * f; v[i][3] = hi.y * f;
+    for (int k = 0; k < 4; ++k) {
+        const float4 f = *reinterpret_cast<const float4 *>(&row_scale[warp * 16 + 4 * k]);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) a[j] = fmaxf(a[j], finite_abs(v[i][j]));
+        for (int j = 0; j < 4; ++j) {
+            float2 x, y;
+            values(t[j][k], f, x, y);
+            a[j] = fmaxf(fmaxf(a[j], fmaxf(fabsf(x.x), fabsf(x.y))), fmaxf(fabsf(y.x), fabsf(y.y)));
+        }
+    }
+    // a value can be infinite where its scale is 2^120 or more, or stands for NaN; such values do not count and become NaN
+    const bool rare = __syncthreads_or(isinf(a[0]) || isinf(a[1]) || isinf(a[2]) || isinf(a[3]));
+    if (rare) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) a[j] = 0.f;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const float4 f = *reinterpret_cast<const float4 *>(&row_scale[warp * 16 + 4 * k]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                float2 x, y;
+                values(t[j][k], f, x, y);
+                a[j] = fmaxf(fmaxf(a[j], fmaxf(finite_abs(x.x), finite_abs(x.y))), fmaxf(finite_abs(y.x), finite_abs(y.y)));
+            }
+        }
     }
     *reinterpret_cast<float4 *>(&most[warp][4 * g]) = make_float4(a[0], a[1], a[2], a[3]);
     __syncthreads();
-#pragma unroll
-    for (int j = 0; j < 4; ++j) a[j] = 0.f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const float4 m = *reinterpret_cast<const float4 *>(&most[i][4 * g]);
         a[0] = fmaxf(a[0], m.x); a[1] = fmaxf(a[1], m.y); a[2] = fmaxf(a[2], m.z); a[3] = fmaxf(a[3], m.w);
     }
+    float inv[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         const unsigned b = scale_byte(a[j]);
-        const float inv = inverse_scale(b);
-        unsigned u[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            u[i] = to_e4m3x2(v[4 * i][j] * inv, v[4 * i + 1][j] * inv) | (to_e4m3x2(v[4 * i + 2][j] * inv, v[4 * i + 3][j] * inv) << 16);
-        tile[(4 * g + j) * 8 + (warp ^ (g & 7))] = make_uint4(u[0], u[1], u[2], u[3]);
+        inv[j] = inverse_scale(b);
         if (warp == 0 && c + j < width) oscale[(int64_t)(c + j) * oss + tr] = (uint8_t)b;
     }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const float4 f = *reinterpret_cast<const float4 *>(&row_scale[warp * 16 + 4 * k]);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            float2 x, y;
+            values(t[j][k], f, x, y);
+            if (rare) { x.x = no_infinity(x.x); x.y = no_infinity(x.y); y.x = no_infinity(y.x); y.y = no_infinity(y.y); }
+            const float2 n = make_float2(inv[j], inv[j]);
+            x = __fmul2_rn(x, n);
+            y = __fmul2_rn(y, n);
+            t[j][k] = to_e4m3x2(x.x, x.y) | (to_e4m3x2(y.x, y.y) << 16);
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) tile[(4 * g + j) * 8 + (warp ^ (g & 7))] = make_uint4(t[j][0], t[j][1], t[j][2], t[j][3]);
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -181,18 +277,19 @@ tad_repack8_kernel(const uint8_t *__restrict__ q, int64_t qs, const uint8_t *__r
         if (at + 16 <= n_rows) *reinterpret_cast<uint4 *>(to) = p;
         else {
             const unsigned words[4] = {p.x, p.y, p.z, p.w};
-            for (int j = 0; j < 16 && at + j < n_rows; ++j) to[j] = (uint8_t)(words[j >> 2] >> (8 * (j & 3)));
+#pragma unroll
+            for (int j = 0; j < 16; ++j) if (at + j < n_rows) to[j] = (uint8_t)(words[j >> 2] >> (8 * (j & 3)));
         }
     }
 }
 
-struct Launch { unsigned blocks, chunks; int cb_log; };
-Launch cover(int64_t n_rows, int64_t n_blocks)
+struct Launch { unsigned blocks, chunks; int cb; };
+Launch cover(int64_t n_rows, int64_t n_blocks, int own)
 {
     Launch l{0, 0, 0};
-    while (l.cb_log < 4 && (int64_t(1) << l.cb_log) < n_blocks) ++l.cb_log;
-    l.chunks = (unsigned)((n_blocks + (1 << l.cb_log) - 1) >> l.cb_log);
-    const int64_t rows = ROWS * (16 >> l.cb_log);
+    while ((NT >> own >> l.cb) > 1 && (int64_t(1) << l.cb) < n_blocks) ++l.cb;
+    l.chunks = (unsigned)((n_blocks + (1 << l.cb) - 1) >> l.cb);
+    const int64_t rows = ROWS * (NT >> own >> l.cb);
     l.blocks = (unsigned)((n_rows + rows - 1) / rows * l.chunks);
     return l;
 }
@@ -202,13 +299,12 @@ Launch cover(int64_t n_rows, int64_t n_blocks)
 // also called by the layer norm for a checkpoint that its own pass cannot write
 tad_status tad_launch_pack8(const tad_rows *x, int64_t n_rows, int64_t width, const tad_packed *out, cudaStream_t stream)
 {
-    const Launch l = cover(n_rows, tadr::blocks_of(width));
+    const bool eights = by_eights(x);
+    const Launch l = cover(n_rows, tadr::blocks_of(width), eights ? OWN_PACK : OWN_ODD);
     cudaError_t e = cudaSuccess;
-    const bool vec = by_eights(x);
     TAD_WITH_TYPE(x->type, T,
-        auto kernel = vec ? tad_pack8_kernel<T, true> : tad_pack8_kernel<T, false>;
-        e = tad_launch(kernel, l.blocks, NT, 0, stream, static_cast<const T *>(x->data), x->stride, n_rows, (int)width,
-                       (int)tadr::blocks_of(width), l.cb_log, l.chunks, out->q, out->q_stride, out->scale, out->scale_stride));
+        e = tad_launch(eights ? tad_pack8_kernel<T> : tad_pack8_odd_kernel<T>, l.blocks, NT, 0, stream, static_cast<const T *>(x->data), x->stride, n_rows, (int)width,
+                       l.cb, l.chunks, out->q, out->q_stride, out->scale, out->scale_stride));
     return launched("pack", e);
 }
 
@@ -227,13 +323,12 @@ tad_status tad_unpack8(const tad_packed *in, int64_t n_rows, int64_t width, cons
     tad_status st;
     if ((st = check_sizes("unpack8", n_rows, width)) || (st = check_packed("unpack8: in", in, n_rows, width)) || (st = check_rows("unpack8: x", x, n_rows, width))) return st;
     if (n_rows == 0 || width == 0) return TAD_OK;
-    const Launch l = cover(n_rows, blocks_of(width));
+    const bool eights = by_eights(x);
+    const Launch l = cover(n_rows, blocks_of(width), eights ? OWN_UNPACK : OWN_ODD);
     cudaError_t e = cudaSuccess;
-    const bool vec = by_eights(x);
     TAD_WITH_TYPE(x->type, T,
-        auto kernel = vec ? tad_unpack8_kernel<T, true> : tad_unpack8_kernel<T, false>;
-        e = tad_launch(kernel, l.blocks, NT, 0, (cudaStream_t)cuda_stream, in->q, in->q_stride, in->scale, in->scale_stride, n_rows, (int)width,
-                       l.cb_log, l.chunks, static_cast<T *>(x->data), x->stride));
+        e = tad_launch(eights ? tad_unpack8_kernel<T> : tad_unpack8_odd_kernel<T>, l.blocks, NT, 0, (cudaStream_t)cuda_stream, in->q, in->q_stride, in->scale, in->scale_stride,
+                       n_rows, (int)width, l.cb, l.chunks, static_cast<T *>(x->data), x->stride));
     return launched("unpack", e);
 }
 
