@@ -335,7 +335,7 @@ tad_status tad_repack8(const tad_packed *in, int64_t n_rows, int64_t width, cons
  * rstd = 1 / sqrt(sum (x - mean)^2 / width + eps), statistics in fp32.
  *   weight, bias   vectors of `width` elements; NULL = ones, zeros
  *   mean, rstd     n_rows floats each, what the backward pass needs; NULL = not wanted
- *   checkpoint     NULL, or x in 8 bits exactly as tad_pack8 gives it, written in the same pass
+ *   checkpoint     NULL, or x in 8 bits exactly as tad_pack8 gives it
  * y may have another type than x.
  * tad_layernorm_backward:  with xh = (x - mean) rstd and g = dy weight,
  *     dx = rstd (g - mean(g) - xh mean(g xh)),   dweight = sum over rows of dy xh,   dbias = sum over rows of dy.

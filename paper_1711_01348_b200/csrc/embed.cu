@@ -7,7 +7,8 @@
 // order, so the sums have a fixed order without atomics.
 //
 // Both directions move bytes and are bound by memory: the gradient reads dy once (rows in sorted order, whole rows at a time)
-// and writes the table's gradient once, zeros included.
+// and writes the table's gradient once, zeros included.  Sorting is a chain of short steps that needs few SMs, so the rows that have
+// no token get their zeros meanwhile; a third kernel adds up the others, a fourth what its warps left in parts.
 #include <cooperative_groups.h>
 
 #include <atomic>
@@ -72,15 +73,17 @@ tad_embed_forward_kernel(const Tokens tok, int64_t n, const S *__restrict__ tabl
 // ---- the sort ----
 
 // One cluster of blocks sorts (key, position) by digits of at most nine bits, least digit first.  A warp owns a run of consecutive
-// elements and counts its digits in shared memory (lanes with equal digits find each other by a vote, one of them adds); the
-// counts of a digit are prefixed over the warps of a block, the blocks of the cluster (read from each other's shared memory) and the
-// digits; then the warp walks its run again and every element knows its place.  One launch for the whole sort, a cluster
-// barrier where a grid of independent blocks would need a launch: the arrays stay in L2.
-constexpr int SORT_NT = 1024, SORT_WARPS = SORT_NT / 32, DIGITS = 512;
+// elements and counts its digits in shared memory; the counts of a digit are prefixed over the warps of a block, the blocks of the
+// cluster (read from each other's shared memory) and the digits; then the warp walks its run again and every element knows its
+// place: lanes with equal digits find each other by a vote for each bit (one instruction that matches all values takes as long as
+// there are values).  One launch for the whole sort, a cluster barrier where a grid of independent blocks would need a launch:
+// the arrays stay in L2.  What bounds it is that and the scattered stores, a key and its position at a time.
+constexpr int SORT_NT = 1024, SORT_WARPS = SORT_NT / 32, DIGIT_BITS = 9, DIGITS = 1 << DIGIT_BITS;
 constexpr size_t SORT_SMEM = SORT_WARPS * DIGITS * 4;
 
-__global__ void __launch_bounds__(SORT_NT)
-tad_embed_sort_kernel(const Tokens tok, unsigned n, unsigned run, int passes, int bits, unsigned *k0, unsigned *p0, unsigned *k1, unsigned *p1)
+// (32 registers a thread: a block of the kernel below fits beside it on an SM)
+__global__ void __launch_bounds__(SORT_NT, 2)
+tad_embed_sort_kernel(const Tokens tok, const unsigned n, const unsigned run, const int passes, const int bits, uint2 *s0, uint2 *s1)
 {
     namespace cg = cooperative_groups;
     extern __shared__ unsigned counts[];                       // of a warp: counts[warp * DIGITS + digit]
@@ -94,31 +97,27 @@ tad_embed_sort_kernel(const Tokens tok, unsigned n, unsigned run, int passes, in
     unsigned *mine = counts + warp * DIGITS;
     tad_wait_previous();
     for (int pass = 0; pass < passes; ++pass) {
-        const unsigned *ki = pass & 1 ? k0 : k1, *pi = pass & 1 ? p0 : p1;
-        unsigned *ko = pass & 1 ? k1 : k0, *po = pass & 1 ? p1 : p0;
+        const uint2 *in = pass & 1 ? s0 : s1;
+        uint2 *out = pass & 1 ? s1 : s0;
         const int shift = pass * bits;
         // (written by other blocks of the cluster in the pass before: not from the first-level cache)
-        auto key_at = [&](unsigned t) { return pass == 0 ? tok.key(t) : __ldcg(ki + t); };
+        auto at = [&](unsigned t) { return pass == 0 ? make_uint2(tok.key(t), t) : __ldcg(in + t); };
         for (int d = lane; d < digits; d += 32) mine[d] = 0;
         __syncwarp();
-        for (unsigned t0 = beg; t0 < end; t0 += 32) {
-            const unsigned t = t0 + lane;
-            const bool live = t < end;
-            const unsigned d = live ? (key_at(t) >> shift) & (digits - 1) : 0xffffffffu;
-            const unsigned same = __match_any_sync(0xffffffffu, d);
-            if (live && (same & ((1u << lane) - 1)) == 0) mine[d] += __popc(same);
-            __syncwarp();
-        }
+#pragma unroll 4
+        for (unsigned t = beg + lane; t < end; t += 32) atomicAdd(&mine[(at(t).x >> shift) & (digits - 1)], 1u);
         __syncthreads();
         const int d = threadIdx.x;
         if (d < digits) {
             unsigned a = 0;
+#pragma unroll 8
             for (int w = 0; w < SORT_WARPS; ++w) { const unsigned c = counts[w * DIGITS + d]; counts[w * DIGITS + d] = a; a += c; }
             total[d] = a;
         }
         cluster.sync();
         unsigned before = 0, all = 0;
         if (d < digits)
+#pragma unroll 8
             for (unsigned b = 0; b < blocks; ++b) {
                 const unsigned c = cluster.map_shared_rank(total, b)[d];
                 if (b < rank) before += c;
@@ -135,74 +134,108 @@ tad_embed_sort_kernel(const Tokens tok, unsigned n, unsigned run, int passes, in
         for (int o = 16; o; o >>= 1) base += __shfl_xor_sync(0xffffffffu, base, o);
         base += up - all + before;
         if (d < digits)
+#pragma unroll 8
             for (int w = 0; w < SORT_WARPS; ++w) counts[w * DIGITS + d] += base;
         __syncthreads();
+        uint2 next = beg + lane < end ? at(beg + lane) : make_uint2(0, 0);
         for (unsigned t0 = beg; t0 < end; t0 += 32) {
-            const unsigned t = t0 + lane;
-            const bool live = t < end;
-            const unsigned key = live ? key_at(t) : 0;
-            const unsigned e = live ? (key >> shift) & (digits - 1) : 0xffffffffu;
-            const unsigned same = __match_any_sync(0xffffffffu, e);
-            const unsigned lower = __popc(same & ((1u << lane) - 1));
-            if (live) {
-                const unsigned to = mine[e] + lower;
-                ko[to] = key;
-                po[to] = pass == 0 ? t : __ldcg(pi + t);
+            const bool live = t0 + lane < end;
+            const uint2 e = next;
+            if (t0 + 32 + lane < end) next = at(t0 + 32 + lane);
+            const unsigned digit = (e.x >> shift) & (digits - 1);
+            unsigned same = __ballot_sync(0xffffffffu, live);
+#pragma unroll
+            for (int b = 0; b < DIGIT_BITS; ++b) {             // (bits behind the digit's are zero in all lanes)
+                const bool one = digit >> b & 1;
+                const unsigned ones = __ballot_sync(0xffffffffu, one);
+                same &= one ? ones : ~ones;
             }
+            const unsigned lower = __popc(same & ((1u << lane) - 1));
+            if (live) out[mine[digit] + lower] = e;
             __syncwarp();
-            if (live && lower == 0) mine[e] += __popc(same);
+            if (live && lower == 0) mine[digit] += __popc(same);
             __syncwarp();
         }
         cluster.sync();
     }
 }
 
+// ---- zeros ----
+
+// Zeros into the rows that no token names, a share of consecutive rows a block.  The block reads all tokens for that: 4 bytes a token and
+// block out of L2, next to the share's rows themselves.  It runs beside the sort, which has waited for the kernels before both
+// by the time that this one starts (its blocks let it start behind their own wait), and waits for the sort at its end, so
+// that who waits for this kernel has waited for both.
+constexpr int CLEAR_NT = 1024;
+constexpr unsigned MAP_ROWS = 32768;                           // rows whose use is noted at a time, a bit each
+
+__global__ void __launch_bounds__(CLEAR_NT)
+tad_embed_clear_kernel(const Tokens tok, const unsigned n, const int64_t each, unsigned char *dtable, const int64_t stride, const int64_t row_bytes, const int piece,
+                       const bool beside)
+{
+    __shared__ unsigned map[MAP_ROWS / 32];
+    if (!beside) tad_wait_previous();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int64_t first = blockIdx.x * each, last = min(first + each, (int64_t)tok.n_table);
+    for (int64_t r0 = first; r0 < last; r0 += MAP_ROWS) {
+        const unsigned rows = (unsigned)min((int64_t)MAP_ROWS, last - r0);
+        __syncthreads();
+        for (unsigned i = threadIdx.x; i < (rows + 31) / 32; i += CLEAR_NT) map[i] = 0;
+        __syncthreads();
+#pragma unroll 4
+        for (int64_t t = threadIdx.x; t < n; t += CLEAR_NT) {
+            const int64_t at = (int64_t)tok.key(t) - r0;
+            if (at >= 0 && at < rows) {
+                const unsigned bit = 1u << (at & 31);
+                if (!(*(volatile unsigned *)&map[at >> 5] & bit)) atomicOr(&map[at >> 5], bit);
+            }
+        }
+        __syncthreads();
+        for (unsigned i = warp; i < rows; i += CLEAR_NT / 32) {
+            if (map[i >> 5] >> (i & 31) & 1) continue;
+            unsigned char *to = dtable + (r0 + i) * stride;
+            if (piece == 32)
+                for (int64_t b = lane * 32; b < row_bytes; b += 1024)
+                    asm volatile("st.global.v8.b32 [%0], {%1,%1,%1,%1,%1,%1,%1,%1};" ::"l"(to + b), "r"(0) : "memory");
+            else if (piece == 4)
+                for (int64_t b = lane * 4; b < row_bytes; b += 128) *reinterpret_cast<unsigned *>(to + b) = 0;
+            else
+                for (int64_t b = lane * 2; b < row_bytes; b += 64) *reinterpret_cast<unsigned short *>(to + b) = 0;
+        }
+    }
+    if (beside) tad_wait_previous();
+}
+
 // ---- the sums ----
 
-// Row ends 0 .. n_table - 1 and sorted tokens are merged into one list (the tokens of a row before its end) that is cut into segments of
-// equal length, so neither a table much longer than the batch nor a token that is half of the batch leaves warps idle.  A warp
-// owns a segment in 256 columns: a token adds its row of dy to the registers, a row end writes them.  A row that
-// begins in one segment and ends in another leaves a partial sum in each: `tail` of the segments that it does not end in, `head` of
-// the one it ends in; tad_embed_join_kernel adds them up in order.
-constexpr int SLICE = 256, AHEAD = 4;
+// The sorted tokens are cut into segments of equal length, so a token that is half of the batch leaves no warps idle.  A warp owns a
+// segment in 256 columns and adds up the rows of dy of one token after the other.  A token whose positions begin in one segment
+// and end in another leaves a partial sum in each: `tail` of the segments that it does not end in, `head` of the one it ends in;
+// tad_embed_join_kernel adds them up in order.
+constexpr int SLICE = 256;
+// rows of dy that a warp has under way: as many as three blocks an SM have registers for
+template <class T, int V> constexpr int AHEAD = V == 8 && sizeof(T) == 2 ? 8 : 4;
+constexpr int SUM_BLOCKS = 3;
 
 struct Cut {
-    unsigned first_row;      // the row that is open at the segment's begin
-    unsigned state;          // OPEN: tokens of it lie in segments before;  ENDS: it ends in this segment
+    unsigned first_row;      // the token that the segment begins with
+    unsigned state;          // OPEN: positions of it lie in segments before;  ENDS: its last one lies in this segment
 };
 constexpr unsigned OPEN = 1, ENDS = 2;
 
 struct Sums {
-    const unsigned *keys, *at;
+    const uint2 *sorted;                                   // token, position
     const void *dy;
     int64_t dys;
     void *dtable;
     int64_t ds;
     int type, accumulate;
-    unsigned n, n_table, segments, slices;
-    int64_t each;            // length of a segment
+    unsigned n, n_table, segments, slices, each;           // each: positions of a segment
     int width;
     float factor;
     float *head, *tail;
     Cut *cuts;
 };
-
-// tokens among the first d entries of the merged list: the first i with keys[i] > d - 1 - i, by the lanes of a warp at once
-__device__ __forceinline__ unsigned tokens_before(const unsigned *__restrict__ keys, unsigned n, unsigned n_table, int64_t d)
-{
-    const int lane = threadIdx.x & 31;
-    int64_t lo = d > n_table ? d - n_table : 0, hi = d < (int64_t)n ? d : (int64_t)n;          // the answer lies in [lo, hi]
-    while (lo < hi) {
-        const int64_t step = (hi - lo + 31) / 32, i = lo + lane * step;
-        const bool before = i < hi && (int64_t)keys[i] <= d - 1 - i;
-        const int k = __popc(__ballot_sync(0xffffffffu, before));                             // (true for the first k lanes)
-        if (k == 0) return (unsigned)lo;
-        const int64_t low = lo + (k - 1) * step + 1;
-        hi = lo + k * step < hi ? lo + k * step : hi;
-        lo = low;
-    }
-    return (unsigned)lo;
-}
 
 // V = 8: a lane's columns are neighbours; V = 1: 32 apart
 template <int V> __device__ __forceinline__ int column_of(int lane, int i) { return V == 8 ? lane * 8 : lane + 32 * i; }
@@ -232,9 +265,8 @@ struct RowPiece {
 
 // the finished sum of a row
 template <int V>
-__device__ __forceinline__ void write_row(const Sums &P, unsigned row, int c0, int lane, int columns, const float (&a)[8], bool any)
+__device__ __forceinline__ void write_row(const Sums &P, unsigned row, int c0, int lane, int columns, const float (&a)[8])
 {
-    if (P.accumulate && !any) return;
     const int64_t at = (int64_t)row * P.ds + c0;
 #pragma unroll
     for (int i = 0; i < 8 / V; ++i) {
@@ -242,7 +274,7 @@ __device__ __forceinline__ void write_row(const Sums &P, unsigned row, int c0, i
         if (c >= columns) continue;
         float v[V];
 #pragma unroll
-        for (int j = 0; j < V; ++j) v[j] = any ? a[i * V + j] * P.factor : 0.f;
+        for (int j = 0; j < V; ++j) v[j] = a[i * V + j] * P.factor;
         auto store = [&](auto *out) {
             using O = typename std::remove_pointer<decltype(out)>::type;
             Piece<O, V> o;
@@ -271,148 +303,161 @@ __device__ __forceinline__ void put_part(float *to, size_t place, int lane, cons
 }
 
 template <class T, int V>
-__global__ void __launch_bounds__(NT)
+__global__ void __launch_bounds__(NT, SUM_BLOCKS)
 tad_embed_sums_kernel(const Sums P)
 {
+    constexpr int A = AHEAD<T, V>;
     tad_wait_previous();
     const int lane = threadIdx.x & 31;
-    const int64_t unit = (int64_t)blockIdx.x * (NT / 32) + (threadIdx.x >> 5);
-    const unsigned s = (unsigned)(unit / P.slices), slice = (unsigned)(unit - (int64_t)s * P.slices);
+    const unsigned unit = blockIdx.x * (NT / 32) + (threadIdx.x >> 5), s = unit / P.slices, slice = unit - s * P.slices;
     if (s >= P.segments) return;
     const int c0 = (int)slice * SLICE, columns = min(SLICE, P.width - c0);
-    const int64_t items = (int64_t)P.n + P.n_table, d0 = s * P.each, d1 = min(items, d0 + P.each);
-    if (d0 >= items) {
-        if (slice == 0 && lane == 0) P.cuts[s] = Cut{P.n_table, 0};
-        return;
-    }
-    unsigned i = tokens_before(P.keys, P.n, P.n_table, d0), j = (unsigned)(d0 - i);
-    const unsigned first = j;
-    bool open = i > 0 && j < P.n_table && P.keys[i - 1] == j, ends = false, any = false;
+    const unsigned beg = (unsigned)min((unsigned long long)P.n, (unsigned long long)s * P.each), end = (unsigned)min((unsigned long long)P.n, (unsigned long long)beg + P.each);
+    unsigned row = beg < end ? P.sorted[beg].x : P.n_table;
+    const unsigned first = row;
+    bool open = beg > 0 && row < P.n_table && P.sorted[beg - 1].x == row, ends = false;
     const bool opened = open;
     const T *__restrict__ dy = static_cast<const T *>(P.dy) + c0;
     float a[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) a[e] = 0.f;
-    int64_t left = d1 - d0;
-    auto end_row = [&] {
+    // the sum of `row` is complete
+    auto close = [&] {
         if (open) {
             put_part(P.head, (size_t)s * P.slices + slice, lane, a);
             ends = true;
             open = false;
-        } else write_row<V>(P, j, c0, lane, columns, a, any);
+        } else write_row<V>(P, row, c0, lane, columns, a);
 #pragma unroll
         for (int e = 0; e < 8; ++e) a[e] = 0.f;
-        any = false;
-        ++j;
-        --left;
     };
-    while (left > 0 && j < P.n_table) {
-        // the next 32 tokens; behind the last one the keys of no row
-        const unsigned key = i + lane < P.n ? P.keys[i + lane] : 0xffffffffu;
-        const unsigned at = i + lane < P.n ? P.at[i + lane] : 0;
-        unsigned used = 0;
-        while (left > 0 && j < P.n_table && used < 32) {
-            // AHEAD tokens of this segment, their rows under way before the first is added
-            RowPiece<T, V> p[AHEAD];
-            unsigned k[AHEAD];
+    // (tokens outside the table are sorted to the end)
+    auto positions = [&](unsigned i) { return i < end ? P.sorted[i] : make_uint2(P.n_table, 0); };
+    uint2 next = positions(beg + lane);
+    for (unsigned i = beg; i < end && row < P.n_table; i += 32) {
+        const uint2 here = next;
+        next = positions(i + 32 + lane);
+        const int count = (int)min(32u, end - i);
+#pragma unroll 1
+        for (int u = 0; u < count; u += A) {
+            // some positions, their rows under way before the first is added
+            RowPiece<T, V> p[A];
+            unsigned k[A];
 #pragma unroll
-            for (int q = 0; q < AHEAD; ++q) {
-                k[q] = __shfl_sync(0xffffffffu, key, used + q);
-                const unsigned t = __shfl_sync(0xffffffffu, at, used + q);
-                const bool here = k[q] < P.n_table && (int64_t)q + (k[q] - j) < left;        // (row ends up to it and tokens before it)
-                p[q].load(dy + (int64_t)t * P.dys, lane, here ? columns : 0);
+            for (int q = 0; q < A; ++q) {
+                k[q] = __shfl_sync(0xffffffffu, here.x, u + q);
+                const unsigned t = __shfl_sync(0xffffffffu, here.y, u + q);
+                p[q].load(dy + (int64_t)t * P.dys, lane, k[q] < P.n_table ? columns : 0);
             }
 #pragma unroll
-            for (int q = 0; q < AHEAD; ++q) {
-                const unsigned stop = min(k[q], P.n_table);
-                while (left > 0 && j < stop) end_row();
-                if (left > 0 && j < P.n_table) {
-                    p[q].add_to(a);
-                    any = true;
-                    ++used;
-                    --left;
+            for (int q = 0; q < A; ++q) {
+                if (k[q] != row) {
+                    if (row < P.n_table && u + q < count) close();
+                    if (u + q < count) row = k[q];
                 }
+                p[q].add_to(a);
             }
         }
-        i += used;
     }
     // the row that is open at the end
-    if (any) put_part(P.tail, (size_t)s * P.slices + slice, lane, a);
+    if (row < P.n_table) {
+        if (end < P.n && P.sorted[end].x == row) put_part(P.tail, (size_t)s * P.slices + slice, lane, a);
+        else close();
+    }
     if (slice == 0 && lane == 0) P.cuts[s] = Cut{first, (opened ? OPEN : 0u) | (ends ? ENDS : 0u)};
 }
 
-// One block a segment: the row that ends here and began in an earlier segment is the sum of the tails from there on and this segment's head.
+// The token that ends in segment s and began in an earlier one is the sum of the tails from there on and the head of s.  A warp a segment
+// and slice; where there are many tails, the warps of the block share them.
+constexpr unsigned MANY = 16;
+
 template <int V>
 __global__ void __launch_bounds__(NT)
 tad_embed_join_kernel(const Sums P)
 {
-    __shared__ float part[NT / 32][SLICE];
+    constexpr int WARPS = NT / 32;
+    __shared__ float part[WARPS][SLICE];
+    __shared__ unsigned shared_first[WARPS];                   // where the block shares the work: the segment that the row begins in
     tad_wait_previous();
-    const unsigned s = blockIdx.x;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const Cut cut = P.cuts[s];
-    if (cut.state != (OPEN | ENDS)) return;
-    // the segment that the row begins in: the last one before s that does not begin inside it
-    unsigned b = s;
-    for (;;) {
-        const bool inside = b > lane && P.cuts[b - 1 - lane].state == OPEN && P.cuts[b - 1 - lane].first_row == cut.first_row;
-        const unsigned k = __ffs(~__ballot_sync(0xffffffffu, inside)) - 1;                  // (all 32 inside: 0xffffffff)
-        if (k < 32) { b -= k + 1; break; }
-        b -= 32;
-    }
-    const unsigned count = s - b;                              // tails of the segments b .. s - 1
-    for (unsigned slice = 0; slice < P.slices; ++slice) {
-        const int c0 = (int)slice * SLICE, columns = min(SLICE, P.width - c0);
-        float a[8];
+    auto add = [&](float (&a)[8], unsigned lo, unsigned hi, unsigned s, unsigned slice) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) a[e] = 0.f;
-        const unsigned lo = (unsigned)((unsigned long long)count * warp / (NT / 32)), hi = (unsigned)((unsigned long long)count * (warp + 1) / (NT / 32));
 #pragma unroll 4
-        for (unsigned q = b + lo; q < b + hi; ++q) {
+        for (unsigned q = lo; q < hi; ++q) {
             Piece<float, 8> p;
             float v[8];
-            p.load(P.tail + ((size_t)q * P.slices + slice) * SLICE + lane * 8);
+            p.load((q < s ? P.tail : P.head) + ((size_t)q * P.slices + slice) * SLICE + lane * 8);
             p.get(v);
 #pragma unroll
             for (int e = 0; e < 8; ++e) a[e] += v[e];
         }
-        __syncthreads();
+    };
+    const unsigned unit0 = blockIdx.x * WARPS, unit = unit0 + warp, s = unit / P.slices, slice = unit - s * P.slices;
+    const Cut cut = s < P.segments ? P.cuts[s] : Cut{0, 0};
+    bool many = false;
+    float a[8];
+    if (cut.state == (OPEN | ENDS)) {
+        // the segment that the row begins in: the last one before s that does not begin inside it
+        unsigned b = s;
+        for (;;) {
+            const bool inside = b > lane && P.cuts[b - 1 - lane].state == OPEN && P.cuts[b - 1 - lane].first_row == cut.first_row;
+            const unsigned k = __ffs(~__ballot_sync(0xffffffffu, inside)) - 1;              // (all 32 inside: 0xffffffff)
+            if (k < 32) { b -= k + 1; break; }
+            b -= 32;
+        }
+        many = s - b > MANY;
+        if (many) { if (lane == 0) shared_first[warp] = b; }
+        else {
+            add(a, b, s + 1, s, slice);
+            write_row<V>(P, cut.first_row, (int)slice * SLICE, lane, min(SLICE, P.width - (int)slice * SLICE), a);
+        }
+    }
+    unsigned todo = 0;
+    if (!__syncthreads_or(many)) return;
+    __shared__ unsigned flags[WARPS];
+    if (lane == 0) flags[warp] = many;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < WARPS; ++w) todo |= flags[w] << w;
+    for (int w = 0; w < WARPS; ++w) {
+        if (!(todo >> w & 1)) continue;
+        const unsigned su = (unit0 + w) / P.slices, sl = unit0 + w - su * P.slices, b = shared_first[w];
+        const unsigned long long count = su + 1 - b;
+        add(a, b + (unsigned)(count * warp / WARPS), b + (unsigned)(count * (warp + 1) / WARPS), su, sl);
 #pragma unroll
         for (int e = 0; e < 8; ++e) part[warp][lane * 8 + e] = a[e];
         __syncthreads();
-        if (warp != 0) continue;
-        for (int w = 1; w < NT / 32; ++w)
+        if (warp == 0) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) a[e] += part[w][lane * 8 + e];
-        Piece<float, 8> p;
-        float v[8];
-        p.load(P.head + ((size_t)s * P.slices + slice) * SLICE + lane * 8);
-        p.get(v);
+            for (int q = 1; q < WARPS; ++q)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) a[e] += v[e];
-        write_row<V>(P, cut.first_row, c0, lane, columns, a, true);
+                for (int e = 0; e < 8; ++e) a[e] += part[q][lane * 8 + e];
+            write_row<V>(P, P.cuts[su].first_row, (int)sl * SLICE, lane, min(SLICE, P.width - (int)sl * SLICE), a);
+        }
+        __syncthreads();
     }
 }
 
 // ---- host ----
 
 struct Layout {
-    unsigned segments, slices;
-    int64_t each;
-    size_t keys, parts, cuts, total;       // bytes of one of the four arrays of the sort, of one plane of partial sums, of the cuts
+    unsigned segments, slices, each;
+    size_t sorted, parts, cuts, total;     // bytes of one of the two arrays of the sort, of one plane of partial sums, of the cuts
 };
-Layout layout_of(int64_t n, int64_t n_table, int64_t width)
+Layout layout_of(int64_t n, int64_t width)
 {
     auto pad = [](size_t b) { return (b + 255) & ~size_t(255); };
     Layout l{};
     l.slices = (unsigned)((width + SLICE - 1) / SLICE);
-    const int64_t items = n + n_table, warps = (int64_t)SMS * 48;
-    l.segments = (unsigned)std::max<int64_t>(1, std::min<int64_t>((items + 15) / 16, (warps + l.slices - 1) / l.slices));
-    l.each = (items + l.segments - 1) / l.segments;
-    l.keys = pad((size_t)n * 4);
+    // warps for all SMs, eight positions each at least (a segment's partial sums cost as much as two)
+    const int64_t warps = (int64_t)SMS * SUM_BLOCKS * (NT / 32), segments = std::max<int64_t>(1, std::min<int64_t>((n + 7) / 8, (warps + l.slices - 1) / l.slices));
+    l.each = (unsigned)((n + segments - 1) / segments);
+    l.segments = (unsigned)((n + l.each - 1) / l.each);
+    l.sorted = pad((size_t)n * sizeof(uint2));
     l.parts = pad((size_t)l.segments * l.slices * SLICE * 4);
     l.cuts = pad((size_t)l.segments * sizeof(Cut));
-    l.total = n > 0 ? 4 * l.keys + 2 * l.parts + l.cuts : 0;
+    l.total = 2 * l.sorted + 2 * l.parts + l.cuts;
     return l;
 }
 
@@ -438,15 +483,6 @@ cudaError_t embed_forward(const Tokens &tok, int64_t n, const tad_rows *table, i
                       static_cast<const S *>(table->data), table->stride, (int)width, factor, static_cast<T *>(y->data), y->stride, log, (unsigned)chunks);
 }
 
-// rows without tokens only
-__global__ void __launch_bounds__(NT)
-tad_embed_zero_kernel(void *out, int type, int64_t stride, int64_t n_rows, int width)
-{
-    tad_wait_previous();
-    for (int64_t r = blockIdx.x; r < n_rows; r += gridDim.x)
-        for (int c = threadIdx.x; c < width; c += NT) put_element(out, type, r * stride + c, 0.f);
-}
-
 }  // namespace
 
 extern "C" {
@@ -467,7 +503,7 @@ tad_status tad_embed_forward(const void *tokens, int32_t token_bits, int64_t n_t
 size_t tad_embed_workspace_bytes(int64_t n_tokens, int64_t n_table, int64_t width)
 {
     if (n_tokens <= 0 || n_table <= 0 || width <= 0 || n_tokens >= MAX_ROWS || n_table >= MAX_ROWS || width >= MAX_WIDTH) return 0;
-    return layout_of(n_tokens, n_table, width).total;
+    return layout_of(n_tokens, width).total;
 }
 
 tad_status tad_embed_backward(const void *tokens, int32_t token_bits, int64_t n_tokens, const tad_rows *dy, int64_t n_table,
@@ -480,45 +516,54 @@ tad_status tad_embed_backward(const void *tokens, int32_t token_bits, int64_t n_
     if ((st = check_room("embed_backward", workspace, workspace_bytes, tad_embed_workspace_bytes(n_tokens, n_table, width)))) return st;
     if (n_table == 0 || width == 0 || (n_tokens == 0 && accumulate)) return TAD_OK;
     const cudaStream_t stream = (cudaStream_t)cuda_stream;
-    if (n_tokens == 0)
-        return launched("embedding gradient", tad_launch(tad_embed_zero_kernel, (unsigned)std::min<int64_t>(n_table, 16 * SMS), NT, 0, stream, dtable->data, (int)dtable->type,
-                                                         dtable->stride, n_table, (int)width));
-    const Layout l = layout_of(n_tokens, n_table, width);
+    const Layout l = n_tokens ? layout_of(n_tokens, width) : Layout{};
     char *ws = static_cast<char *>(workspace);
-    unsigned *k0 = reinterpret_cast<unsigned *>(ws), *p0 = reinterpret_cast<unsigned *>(ws + l.keys), *k1 = reinterpret_cast<unsigned *>(ws + 2 * l.keys),
-             *p1 = reinterpret_cast<unsigned *>(ws + 3 * l.keys);
+    uint2 *s0 = reinterpret_cast<uint2 *>(ws), *s1 = reinterpret_cast<uint2 *>(ws + l.sorted);
+    const Tokens tok{tokens, token_bits, (unsigned)n_table};
     // digits of at most nine bits; keys run to n_table, the key of tokens outside the table
     int key_bits = 1;
     while (((uint64_t)n_table >> key_bits) != 0) ++key_bits;
-    const int passes = (key_bits + 8) / 9, bits = (key_bits + passes - 1) / passes;
-    const int blocks = n_tokens <= 2048 ? 1 : 8;
-    const int64_t warps = (int64_t)blocks * SORT_WARPS, run = ((n_tokens + warps - 1) / warps + 31) / 32 * 32;
-    static std::atomic<bool> allowed[64];
-    int dev = -1;
-    cudaError_t e = cudaGetDevice(&dev);
-    if (e == cudaSuccess && (dev < 0 || dev >= 64 || !allowed[dev].load(std::memory_order_relaxed))) {
-        e = cudaFuncSetAttribute(tad_embed_sort_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)SORT_SMEM);
-        if (e == cudaSuccess && dev >= 0 && dev < 64) allowed[dev].store(true, std::memory_order_relaxed);
+    const int passes = (key_bits + DIGIT_BITS - 1) / DIGIT_BITS, bits = (key_bits + passes - 1) / passes;
+    cudaError_t e = cudaSuccess;
+    if (n_tokens) {
+        static std::atomic<bool> allowed[64];
+        int dev = -1;
+        e = cudaGetDevice(&dev);
+        if (e == cudaSuccess && (dev < 0 || dev >= 64 || !allowed[dev].load(std::memory_order_relaxed))) {
+            e = cudaFuncSetAttribute(tad_embed_sort_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)SORT_SMEM);
+            if (e == cudaSuccess && dev >= 0 && dev < 64) allowed[dev].store(true, std::memory_order_relaxed);
+        }
+        // (sixteen blocks sort 65536 tokens in 22 us for 30, but a cluster of that size delays the kernels around it: the gradient into
+        // 128000 x 2048 363 us for 287)
+        const int cluster = n_tokens <= 2048 ? 1 : 8;
+        const int64_t warps = (int64_t)cluster * SORT_WARPS, run = ((n_tokens + warps - 1) / warps + 31) / 32 * 32;
+        if (e == cudaSuccess)
+            e = tad_launch_cluster(tad_embed_sort_kernel, cluster, SORT_NT, SORT_SMEM, stream, cluster, tok, (unsigned)n_tokens, (unsigned)run, passes, bits, s0, s1);
+        if (e != cudaSuccess) return launched("sort of the tokens", e);
     }
-    if (e == cudaSuccess)
-        e = tad_launch_cluster(tad_embed_sort_kernel, blocks, SORT_NT, SORT_SMEM, stream, blocks, Tokens{tokens, token_bits, (unsigned)n_table},
-                               (unsigned)n_tokens, (unsigned)run, passes, bits, k0, p0, k1, p1);
-    if (e != cudaSuccess) return launched("sort of the tokens", e);
+    if (!accumulate) {
+        const int64_t size = (int64_t)type_size(dtable->type), stride = dtable->stride * size, row_bytes = width * size;
+        auto whole = [&](int64_t b) { return reinterpret_cast<uintptr_t>(dtable->data) % b == 0 && stride % b == 0 && row_bytes % b == 0; };
+        const int64_t blocks = std::min<int64_t>(SMS, (n_table + 31) / 32), each = (n_table + blocks - 1) / blocks;
+        e = tad_launch(tad_embed_clear_kernel, (unsigned)blocks, CLEAR_NT, 0, stream, tok, (unsigned)n_tokens, each, static_cast<unsigned char *>(dtable->data), stride,
+                       row_bytes, whole(32) ? 32 : whole(4) ? 4 : 2, n_tokens > 0);
+        if (e != cudaSuccess || n_tokens == 0) return launched("clearing of rows without tokens", e);
+    }
     Sums P{};
-    P.keys = passes & 1 ? k0 : k1; P.at = passes & 1 ? p0 : p1;
+    P.sorted = passes & 1 ? s0 : s1;
     P.dy = dy->data; P.dys = dy->stride;
     P.dtable = dtable->data; P.ds = dtable->stride; P.type = dtable->type; P.accumulate = accumulate != 0;
     P.n = (unsigned)n_tokens; P.n_table = (unsigned)n_table; P.segments = l.segments; P.slices = l.slices; P.each = l.each;
     P.width = (int)width; P.factor = factor;
-    P.head = reinterpret_cast<float *>(ws + 4 * l.keys); P.tail = reinterpret_cast<float *>(ws + 4 * l.keys + l.parts);
-    P.cuts = reinterpret_cast<Cut *>(ws + 4 * l.keys + 2 * l.parts);
+    P.head = reinterpret_cast<float *>(ws + 2 * l.sorted); P.tail = reinterpret_cast<float *>(ws + 2 * l.sorted + l.parts);
+    P.cuts = reinterpret_cast<Cut *>(ws + 2 * l.sorted + 2 * l.parts);
     const bool eights = width % 8 == 0 && by_eights(dy) && by_eights(dtable);
     const unsigned grid = (unsigned)(((int64_t)l.segments * l.slices + NT / 32 - 1) / (NT / 32));
     TAD_WITH_TYPE(dy->type, T, {
         auto kernel = eights ? tad_embed_sums_kernel<T, 8> : tad_embed_sums_kernel<T, 1>;
         e = tad_launch(kernel, grid, NT, 0, stream, P);
     });
-    if (e == cudaSuccess) e = tad_launch(eights ? tad_embed_join_kernel<8> : tad_embed_join_kernel<1>, l.segments, NT, 0, stream, P);
+    if (e == cudaSuccess && l.segments > 1) e = tad_launch(eights ? tad_embed_join_kernel<8> : tad_embed_join_kernel<1>, grid, NT, 0, stream, P);
     return launched("embedding gradient", e);
 }
 

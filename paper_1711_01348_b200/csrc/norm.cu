@@ -40,8 +40,7 @@ struct Params {
     const void *x, *dy, *w, *b;
     void *y, *dx;
     const uint8_t *q, *scale;
-    uint8_t *kq, *kscale;
-    int64_t xs, dys, ys, dxs, qs, ss, kqs, kss;
+    int64_t xs, dys, ys, dxs, qs, ss;
     float *mean, *rstd, *planes;
     int64_t n_rows;
     int width, w_type, b_type, y_type, dx_type;
@@ -52,39 +51,38 @@ struct Params {
 // How rows are divided: a warp a row, a group of warps, a cluster of groups (a block each).
 enum { BY_WARP, BY_GROUP, BY_CLUSTER };
 
-// A thread's E elements lie in the 32 E columns of its warp: V = 8, pieces of eight, 256 columns apart; V = 16, two of them side by side;
-// V = 1, 32 apart.  So every access of a row is the thread's pointer and a constant.  Piece i exists where place(i) < rem, the columns
-// from the thread's first one to the end of the row.
+// A thread's E elements lie in the 32 E columns of its warp: V = 8, pieces of eight, 256 columns apart; V = 1, 32 apart.  So every access of
+// a row is the thread's pointer and a constant, and the warp's accesses are contiguous.  (Sixteen elements side by side would let eight
+// threads pack a block of 128 for a checkpoint, but their stores of 16 bytes lie 32 apart: 16384 x 2048 bf16 43 us for 36.)  Piece i
+// exists where place(i) < rem, the columns from the thread's first one to the end of the row.
 template <int V> struct Of {
-    static constexpr int PIECE = V == 1 ? 1 : 8;
-    __device__ __forceinline__ static constexpr int place(int i) { return V == 16 ? i * 8 : V == 8 ? i * 256 : i * 32; }
+    __device__ __forceinline__ static constexpr int place(int i) { return V == 8 ? i * 256 : i * 32; }
     // column of element e behind the thread's first
-    __device__ __forceinline__ static constexpr int column(int e) { return place(e / PIECE) + e % PIECE; }
+    __device__ __forceinline__ static constexpr int column(int e) { return place(e / V) + e % V; }
 };
 
 template <class T, int V, int E>
 struct Held {
-    static constexpr int PV = Of<V>::PIECE;
-    Piece<T, PV> p[E / PV];
+    Piece<T, V> p[E / V];
     __device__ __forceinline__ void zero()
     {
 #pragma unroll
-        for (int i = 0; i < E / PV; ++i) p[i].zero();
+        for (int i = 0; i < E / V; ++i) p[i].zero();
     }
     // (pieces that do not exist keep their zeros)
     __device__ __forceinline__ void fetch(const T *__restrict__ at, int rem)
     {
 #pragma unroll
-        for (int i = 0; i < E / PV; ++i) if (Of<V>::place(i) < rem) p[i].load(at + Of<V>::place(i));
+        for (int i = 0; i < E / V; ++i) if (Of<V>::place(i) < rem) p[i].load(at + Of<V>::place(i));
     }
     __device__ __forceinline__ void get(float (&v)[E]) const
     {
 #pragma unroll
-        for (int i = 0; i < E / PV; ++i) {
-            float f[PV];
+        for (int i = 0; i < E / V; ++i) {
+            float f[V];
             p[i].get(f);
 #pragma unroll
-            for (int j = 0; j < PV; ++j) v[i * PV + j] = f[j];
+            for (int j = 0; j < V; ++j) v[i * V + j] = f[j];
         }
     }
 };
@@ -106,7 +104,7 @@ __device__ __forceinline__ void load_vector(float (&v)[E], const void *p, int ty
         for (int e = 0; e < E; ++e) v[e] = none;
     } else if (V != 1 && reinterpret_cast<uintptr_t>(p) % 16 != 0) {
 #pragma unroll
-        for (int e = 0; e < E; ++e) v[e] = Of<V>::place(e / Of<V>::PIECE) < rem ? element(p, type, c + Of<V>::column(e)) : 0.f;
+        for (int e = 0; e < E; ++e) v[e] = Of<V>::place(e / V) < rem ? element(p, type, c + Of<V>::column(e)) : 0.f;
     } else if (type == TAD_F32) load_held<float, V, E>(v, static_cast<const float *>(p) + c, rem);
     else if (type == TAD_BF16) load_held<__nv_bfloat16, V, E>(v, static_cast<const __nv_bfloat16 *>(p) + c, rem);
     else load_held<__half, V, E>(v, static_cast<const __half *>(p) + c, rem);
@@ -115,14 +113,13 @@ __device__ __forceinline__ void load_vector(float (&v)[E], const void *p, int ty
 template <class O, int V, int E>
 __device__ __forceinline__ void store_held(O *at, int rem, const float (&v)[E])
 {
-    constexpr int PV = Of<V>::PIECE;
 #pragma unroll
-    for (int i = 0; i < E / PV; ++i) {
+    for (int i = 0; i < E / V; ++i) {
         if (Of<V>::place(i) >= rem) continue;
-        float f[PV];
+        float f[V];
 #pragma unroll
-        for (int j = 0; j < PV; ++j) f[j] = v[i * PV + j];
-        Piece<O, PV> o;
+        for (int j = 0; j < V; ++j) f[j] = v[i * V + j];
+        Piece<O, V> o;
         o.set(f);
         o.store(at + Of<V>::place(i));
     }
@@ -152,7 +149,7 @@ template <int E> struct Pairs {
 // a value of the pieces that exist, zero behind the row, for elements 2 j and 2 j + 1
 template <int V> __device__ __forceinline__ float2 inside(float v, int j, int rem)
 {
-    return make_float2(Of<V>::place(2 * j / Of<V>::PIECE) < rem ? v : 0.f, Of<V>::place((2 * j + 1) / Of<V>::PIECE) < rem ? v : 0.f);
+    return make_float2(Of<V>::place(2 * j / V) < rem ? v : 0.f, Of<V>::place((2 * j + 1) / V) < rem ? v : 0.f);
 }
 
 __device__ __forceinline__ float warp_sum(float v)
@@ -348,11 +345,11 @@ struct Ring {
 
 // The thread's elements of a row in the ring.  Every thread reads its places, whether they exist or not: those behind the row hold zeros
 // from the start (clear_ring), which costs no selects where the row is read.
-template <class T, int E, int V = 8>
+template <class T, int E>
 __device__ __forceinline__ void read_row(Piece<T, 8> (&p)[E / 8], const T *at)
 {
 #pragma unroll
-    for (int i = 0; i < E / 8; ++i) p[i].load(at + Of<V>::place(i));
+    for (int i = 0; i < E / 8; ++i) p[i].load(at + Of<8>::place(i));
 }
 template <class T, int E>
 __device__ __forceinline__ void elements(float (&v)[E], const Piece<T, 8> (&p)[E / 8])
@@ -376,39 +373,8 @@ __device__ __forceinline__ void clear_ring(unsigned char *rows, unsigned bytes)
 
 template <class T> constexpr int FORWARD_STAGES = sizeof(T) == 2 ? 4 : 2;
 
-// x into 8 bits beside the pass.  16-bit types (V = 16): eight neighbouring threads hold a block of 128, sixteen elements each; fp32 (V = 8):
-// sixteen threads.
-template <class T, int V>
-__device__ __forceinline__ void keep_row(const Params &P, int64_t r, int col, int rem, const Piece<T, 8> (&p)[2])
-{
-    if constexpr (V == 16) {
-        Sixteen<T> x;
-        const unsigned w[8] = {p[0].a.x, p[0].a.y, p[0].a.z, p[0].a.w, p[1].a.x, p[1].a.y, p[1].a.z, p[1].a.w};
-#pragma unroll
-        for (int j = 0; j < 8; ++j) x.w[j] = w[j];
-        unsigned byte;
-        const uint4 q = x.pack(byte);
-        uint8_t *to = P.kq + r * P.kqs + col;
-        if (rem > 8) *reinterpret_cast<uint4 *>(to) = q;
-        else if (rem > 0) *reinterpret_cast<uint2 *>(to) = make_uint2(q.x, q.y);
-        if ((threadIdx.x & 7) == 0 && rem > 0) P.kscale[r * P.kss + col / TAD_BLOCK8] = (uint8_t)byte;
-    } else {
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            float f[8];
-            p[i].get(f);
-            unsigned byte;
-            const uint2 q = pack_block(f, byte);
-            if (Of<V>::place(i) >= rem) continue;
-            const int c = col + Of<V>::place(i);
-            *reinterpret_cast<uint2 *>(P.kq + r * P.kqs + c) = q;
-            if ((threadIdx.x & 15) == 0) P.kscale[r * P.kss + c / TAD_BLOCK8] = (uint8_t)byte;
-        }
-    }
-}
-
-// V = 8, 16: width and all row starts are whole pieces of eight.  KEEP: with the checkpoint.
-template <class T, int V, int BY, bool KEEP>
+// V = 8: width and all row starts are whole pieces of eight.
+template <class T, int V, int BY>
 __global__ void __launch_bounds__(FORWARD_BLOCK, V == 1 ? 2 : FORWARD_BLOCKS)
 tad_norm_forward_kernel(const Params P)
 {
@@ -452,9 +418,8 @@ tad_norm_forward_kernel(const Params P)
         if constexpr (V != 1) {
             ring.wait();
             Piece<T, 8> p[E / 8];
-            read_row<T, E, V>(p, reinterpret_cast<const T *>(ring.row()) + (at.col - at.col0));
+            read_row<T, E>(p, reinterpret_cast<const T *>(ring.row()) + (at.col - at.col0));
             elements<T, E>(v, p);
-            if constexpr (KEEP) keep_row<T, V>(P, r, at.col, at.rem, p);
         } else {
             next.get(v);
             if (r + at.step < P.n_rows) next.fetch(x + (r + at.step) * P.xs + at.col, at.rem);
@@ -873,17 +838,15 @@ int64_t planes_of(int64_t n_rows, int64_t width, int e)
 }
 
 template <class T>
-cudaError_t forward(const Params &P, const Shape &s, bool eights, bool keep, cudaStream_t stream)
+cudaError_t forward(const Params &P, const Shape &s, bool eights, cudaStream_t stream)
 {
     if (P.width > HELD) return tad_launch(tad_norm_forward_long_kernel<T>, (unsigned)std::min<int64_t>(P.n_rows, 2 * SMS), LARGE, 0, stream, P);
     const int threads = s.by == BY_WARP ? FORWARD_BLOCK : s.group, groups = s.by == BY_WARP ? FORWARD_BLOCK / 32 : 1;
     const int64_t most = (int64_t)SMS * std::min(32, (eights ? FORWARD_BLOCKS : 2) * FORWARD_BLOCK / threads) / s.cluster;
     const unsigned blocks = (unsigned)(std::min((P.n_rows + groups - 1) / groups, most) * s.cluster);
-    auto kernel = tad_norm_forward_kernel<T, 1, BY_WARP, false>;
-    constexpr int VK = sizeof(T) == 2 ? 16 : 8;
-    if (eights && keep) kernel = s.by == BY_WARP ? tad_norm_forward_kernel<T, VK, BY_WARP, true> : s.by == BY_GROUP ? tad_norm_forward_kernel<T, VK, BY_GROUP, true> : tad_norm_forward_kernel<T, VK, BY_CLUSTER, true>;
-    else if (eights) kernel = s.by == BY_WARP ? tad_norm_forward_kernel<T, 8, BY_WARP, false> : s.by == BY_GROUP ? tad_norm_forward_kernel<T, 8, BY_GROUP, false> : tad_norm_forward_kernel<T, 8, BY_CLUSTER, false>;
-    else if (s.by != BY_WARP) kernel = s.by == BY_GROUP ? tad_norm_forward_kernel<T, 1, BY_GROUP, false> : tad_norm_forward_kernel<T, 1, BY_CLUSTER, false>;
+    auto kernel = tad_norm_forward_kernel<T, 1, BY_WARP>;
+    if (eights) kernel = s.by == BY_WARP ? tad_norm_forward_kernel<T, 8, BY_WARP> : s.by == BY_GROUP ? tad_norm_forward_kernel<T, 8, BY_GROUP> : tad_norm_forward_kernel<T, 8, BY_CLUSTER>;
+    else if (s.by != BY_WARP) kernel = s.by == BY_GROUP ? tad_norm_forward_kernel<T, 1, BY_GROUP> : tad_norm_forward_kernel<T, 1, BY_CLUSTER>;
     const size_t smem = eights ? (size_t)threads * FORWARD_E * sizeof(T) * FORWARD_STAGES<T> : 0;      // (32 KB at most)
     return tad_launch_cluster(kernel, blocks, threads, smem, stream, s.cluster, P);
 }
@@ -955,11 +918,12 @@ tad_status tad_layernorm_forward(const tad_rows *x, int64_t n_rows, int64_t widt
     P.n_rows = n_rows; P.width = (int)width; P.eps = eps; P.inv_width = 1.f / (float)width;
     const Shape s = shape_of(width, FORWARD_BLOCK, FORWARD_E);
     P.group = s.group;
-    const bool eights = width % 8 == 0 && by_eights(x) && by_eights(y), keep = checkpoint && eights && width <= HELD;
-    if (keep) { P.kq = checkpoint->q; P.kqs = checkpoint->q_stride; P.kscale = checkpoint->scale; P.kss = checkpoint->scale_stride; }
-    else if (checkpoint && (st = tad_launch_pack8(x, n_rows, width, checkpoint, stream))) return st;
+    const bool eights = width % 8 == 0 && by_eights(x) && by_eights(y);
+    // The checkpoint by a pass of its own, which leaves x in L2 for the next one.  In one pass the norm's threads, who hold a row in step, wait
+    // for the packing of every row (16384 x 2048 bf16 43 to 51 us for 41; 8192 x 4096 46 to 55 for 42).
+    if (checkpoint && (st = tad_launch_pack8(x, n_rows, width, checkpoint, stream))) return st;
     cudaError_t e = cudaSuccess;
-    TAD_WITH_TYPE(x->type, T, e = forward<T>(P, s, eights, keep, stream));
+    TAD_WITH_TYPE(x->type, T, e = forward<T>(P, s, eights, stream));
     return launched("layer norm", e);
 }
 

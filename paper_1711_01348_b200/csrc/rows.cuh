@@ -199,36 +199,9 @@ __device__ __forceinline__ float2 from_e4m3x2(unsigned two)
     const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)two, __NV_E4M3);
     return __half22float2(*reinterpret_cast<const __half2 *>(&h));
 }
-__device__ __forceinline__ uint2 pack_eight(const float (&v)[8], float inv)
-{
-    return make_uint2(to_e4m3x2(v[0] * inv, v[1] * inv) | (to_e4m3x2(v[2] * inv, v[3] * inv) << 16),
-                      to_e4m3x2(v[4] * inv, v[5] * inv) | (to_e4m3x2(v[6] * inv, v[7] * inv) << 16));
-}
 // infinities as NaNs: e4m3 has none, and the conversion would make them 448
 __device__ __forceinline__ float no_infinity(float x) { return isinf(x) ? __uint_as_float(0x7fffffffu) : x; }
 
-// Sixteen neighbouring lanes pack a block of 128 (zeros behind the row), eight elements each; byte: the block's scale.  Infinities are
-// looked for once a block: a maximum leaves out NaNs but not them.
-__device__ __forceinline__ uint2 pack_block(float (&v)[8], unsigned &byte)
-{
-    float a = 0.f;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) a = fmaxf(a, fabsf(v[j]));
-#pragma unroll
-    for (int d = 8; d; d >>= 1) a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, d));
-    if (__any_sync(0xffffffffu, isinf(a))) {
-        a = 0.f;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            a = fmaxf(a, finite_abs(v[j]));
-            v[j] = no_infinity(v[j]);
-        }
-#pragma unroll
-        for (int d = 8; d; d >>= 1) a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, d));
-    }
-    byte = scale_byte(a);
-    return pack_eight(v, inverse_scale(byte));
-}
 __device__ __forceinline__ void unpack_eight(uint2 q, float s, float (&v)[8])
 {
     const unsigned h[4] = {q.x & 0xffffu, q.x >> 16, q.y & 0xffffu, q.y >> 16};
