@@ -9,7 +9,9 @@
 // One block an SM, walking over tiles of 128 rows of one operand (p: the lanes of tensor memory) and BN of the other (q).  A warp
 // copies 128 x 128 and BN x 128 bytes a stage by TMA (a block of 128 elements is one 128-byte line of the swizzled layout), four warps
 // bring the scales of 512 elements at a time from memory into tensor memory, a warp issues the MMAs and eight warps empty the
-// accumulator.
+// accumulator.  Large products run on pairs of blocks (PAIR, clusters of two SMs): a tile of 256 x 256, each block holds 128 rows of p and
+// of q and half of the accumulator, and the first block issues the MMAs of both.  What bounds those is L2: at the full rate of the
+// tensor cores single tiles of 128 x 256 would read 27 TB/s from it.
 #include <cuda.h>
 
 #include <atomic>
@@ -21,20 +23,30 @@ namespace {
 using namespace tadr;
 
 constexpr int BM = 128, KB = 128;                 // rows of p in a tile; bytes of a row in a stage (a block of the scales)
-constexpr int SF_BLOCKS = 4;                      // blocks whose scales are one word of tensor memory
-constexpr int EPI_WARPS = 8, SF_WARPS = 4, NT = (EPI_WARPS + SF_WARPS + 2) * 32;
+constexpr int SF_BLOCKS = 4, SF_BUFFERS = 8;      // blocks whose scales are one word of tensor memory (a chunk); chunks in tensor memory
+constexpr int EPI_WARPS = 8, SF_WARPS = 4, NT = 512;
+// registers: 512 threads start with 128 each; the last two warpgroups go down to 56, the two that empty the accumulator up to 200
+constexpr int REG_EPI = 200, REG_REST = 56;
 constexpr long long WAIT_LIMIT = 1ll << 32;       // clocks after which a wait gives up (about two seconds; a tile takes 0.1 s at most)
 constexpr int STAGE_ROOM = 196608;                // shared memory of the stages
 
 // ---- PTX ----
 __device__ __forceinline__ unsigned smem_u32(const void *p) { return (unsigned)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ void mbar_init(unsigned bar, unsigned count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory"); }
+// `bar` of block `rank` of the cluster
+__device__ __forceinline__ unsigned at_block(unsigned bar, unsigned rank)
+{
+    unsigned r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(bar), "r"(rank));
+    return r;
+}
+__device__ __forceinline__ void mbar_arrive_far(unsigned bar) { asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory"); }
 __device__ __forceinline__ void mbar_arrive(unsigned bar) { asm volatile("{ .reg .b64 t; mbarrier.arrive.shared::cta.b64 t, [%0]; }" ::"r"(bar) : "memory"); }
 __device__ __forceinline__ void mbar_expect(unsigned bar, unsigned bytes) { asm volatile("{ .reg .b64 t; mbarrier.arrive.expect_tx.shared::cta.b64 t, [%0], %1; }" ::"r"(bar), "r"(bytes) : "memory"); }
 __device__ __forceinline__ bool mbar_try(unsigned bar, unsigned parity)
 {
     unsigned ok;
-    asm volatile("{ .reg .pred p; mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    asm volatile("{ .reg .pred p; mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
     return ok != 0;
 }
 // (by whole warps) false: this wait ran out, or another one of the block did
@@ -61,15 +73,30 @@ __device__ __forceinline__ void tma_load(unsigned to, const CUtensorMap *map, in
 {
     asm volatile("cp.async.bulk.tensor.2d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(to), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
 }
+// the same by either block of a pair, counted at a barrier of the first one
+__device__ __forceinline__ void tma_load_pair(unsigned to, const CUtensorMap *map, int x, int y, unsigned bar)
+{
+    asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(to), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
+}
 // by a whole warp with uniform operands, one elected lane issues
+template <bool PAIR>
 __device__ __forceinline__ void mma_scaled(unsigned d, unsigned long long a, unsigned long long b, unsigned idesc, unsigned sfa, unsigned sfb, unsigned acc)
 {
-    asm volatile("{ .reg .pred p, q; elect.sync _|q, 0xffffffff; setp.ne.u32 p, %6, 0;\n"
-                 "@q tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p; }" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(acc) : "memory");
+    if (PAIR)
+        asm volatile("{ .reg .pred p, q; elect.sync _|q, 0xffffffff; setp.ne.u32 p, %6, 0;\n"
+                     "@q tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p; }" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(acc) : "memory");
+    else
+        asm volatile("{ .reg .pred p, q; elect.sync _|q, 0xffffffff; setp.ne.u32 p, %6, 0;\n"
+                     "@q tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p; }" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(acc) : "memory");
 }
+// arrives at the barrier (PAIR: of both blocks) when the MMAs so far are done
+template <bool PAIR>
 __device__ __forceinline__ void mma_commit(unsigned bar)
 {
-    asm volatile("{ .reg .pred q; elect.sync _|q, 0xffffffff; @q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0]; }" ::"r"(bar) : "memory");
+    if (PAIR)
+        asm volatile("{ .reg .pred q; .reg .b16 m; mov.b16 m, 3; elect.sync _|q, 0xffffffff; @q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], m; }" ::"r"(bar) : "memory");
+    else
+        asm volatile("{ .reg .pred q; elect.sync _|q, 0xffffffff; @q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0]; }" ::"r"(bar) : "memory");
 }
 __device__ __forceinline__ void tmem_ld32(unsigned addr, float (&v)[32])
 {
@@ -78,10 +105,10 @@ __device__ __forceinline__ void tmem_ld32(unsigned addr, float (&v)[32])
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
                    "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
                  : "r"(addr));
-    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 #pragma unroll
     for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(r[j]);
 }
+__device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_st4(unsigned addr, const unsigned (&r)[4])
 {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
@@ -98,94 +125,128 @@ struct Product {
     void *y;                                      // or the planes of a split product
     int64_t yp, yq;                               // element strides of y along p and q: one of them is 1
     int64_t plane;                                // elements of a plane, 0 without a split
-    int type, vec;                                // vec: sixteen-byte stores along q
+    int type, vec;                                // vec: stores of 32 bytes along q
     int np, nq, blocks, each, split;              // sizes, blocks of k, blocks of a share of k, shares
     unsigned tiles_p, tiles_q, tiles;
 };
 
-template <int BN> struct Config {
-    static constexpr int STAGE = (BM + BN) * KB, STAGES = STAGE_ROOM / STAGE < 8 ? STAGE_ROOM / STAGE : 8;
+template <int BN, bool PAIR> struct Config {
+    static constexpr int ROWS_Q = PAIR ? BN / 2 : BN;                     // rows of q that a block copies
+    static constexpr int STAGE = (BM + ROWS_Q) * KB, STAGES = STAGE_ROOM / STAGE < 8 ? STAGE_ROOM / STAGE : 8;
     static constexpr size_t SMEM = 1024 + (size_t)STAGES * STAGE;
-    static constexpr int SF_Q = (BN + 127) / 128 * 4, SF_COLS = 16;       // columns of q's scales; of a buffer of scales
+    static constexpr int SF_COLS = 16;                                    // columns of a buffer of scales: four of p, up to eight of q
 };
 
 // tiles of one share of k in groups of sixteen along p, so that the blocks that run together share operand lines in L2
-__device__ __forceinline__ void tile_at(const Product &P, unsigned t, int &p0, int &q0, int &share, int bn)
+__device__ __forceinline__ void tile_at(const Product &P, unsigned t, int &p0, int &q0, int &share, int bm, int bn)
 {
     const unsigned per = P.tiles_p * P.tiles_q;
     share = (int)(t / per);
     t -= (unsigned)share * per;
     const unsigned group = 16u * P.tiles_q, g = t / group, first = g * 16u, size = min(16u, P.tiles_p - first), in = t - g * group;
-    p0 = (int)(first + in % size) * BM;
+    p0 = (int)(first + in % size) * bm;
     q0 = (int)(in / size) * bn;
 }
 
-template <int BN>
+// four bytes of results
+template <class T> __device__ __forceinline__ unsigned word_of(const float *v);
+template <> __device__ __forceinline__ unsigned word_of<float>(const float *v) { return __float_as_uint(v[0]); }
+template <> __device__ __forceinline__ unsigned word_of<__nv_bfloat16>(const float *v) { const __nv_bfloat162 h = __floats2bfloat162_rn(v[0], v[1]); return *reinterpret_cast<const unsigned *>(&h); }
+template <> __device__ __forceinline__ unsigned word_of<__half>(const float *v) { const __half2 h = __floats2half2_rn(v[0], v[1]); return *reinterpret_cast<const unsigned *>(&h); }
+
+// all threads of the block or pair
+template <bool PAIR>
+__device__ __forceinline__ void block_sync()
+{
+    if (PAIR) {
+        asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    } else __syncthreads();
+}
+
+template <int BN, bool PAIR>
 __global__ void __launch_bounds__(NT, 1)
 tad_product8_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtensorMap map_q, const Product P)
 {
-    using C = Config<BN>;
-    constexpr int S = C::STAGES;
+    using C = Config<BN, PAIR>;
+    constexpr int S = C::STAGES, TILE_P = PAIR ? 2 * BM : BM;
     extern __shared__ unsigned char smem_raw[];
-    __shared__ unsigned long long bars[2 * S + 6];
-    __shared__ unsigned tmem_base;
+    __shared__ unsigned long long bars[2 * S + 2 * SF_BUFFERS + 2];
+    __shared__ unsigned tmem_base, spread[2][BM + (BN < 128 ? 128 : BN)];
     __shared__ volatile int failed;
     const unsigned smem0 = (smem_u32(smem_raw) + 1023u) & ~1023u;
-    const unsigned full = smem_u32(&bars[0]), empty = full + 8 * S, sf_full = empty + 8 * S, sf_empty = sf_full + 16, acc_full = sf_empty + 16, acc_empty = acc_full + 8;
+    const unsigned full = smem_u32(&bars[0]), empty = full + 8 * S, sf_full = empty + 8 * S, sf_empty = sf_full + 8 * SF_BUFFERS, acc_full = sf_empty + 8 * SF_BUFFERS, acc_empty = acc_full + 8;
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+    const unsigned rank = PAIR ? blockIdx.x & 1 : 0;                      // in the pair; the first block issues the MMAs
+    const unsigned walker = PAIR ? blockIdx.x >> 1 : blockIdx.x, walkers = PAIR ? gridDim.x >> 1 : gridDim.x;
     if (warp == EPI_WARPS) {
         if (lane == 0) {
             failed = 0;
             for (int i = 0; i < S; ++i) { mbar_init(full + 8 * i, 1); mbar_init(empty + 8 * i, 1); }
-            for (int i = 0; i < 2; ++i) { mbar_init(sf_full + 8 * i, SF_WARPS); mbar_init(sf_empty + 8 * i, 1); }
+            for (int i = 0; i < SF_BUFFERS; ++i) { mbar_init(sf_full + 8 * i, PAIR ? 2 * SF_WARPS : SF_WARPS); mbar_init(sf_empty + 8 * i, 1); }
             mbar_init(acc_full, 1);
-            mbar_init(acc_empty, EPI_WARPS);
+            mbar_init(acc_empty, PAIR ? 2 * EPI_WARPS : EPI_WARPS);
             asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         }
         __syncwarp();
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&tmem_base)) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        if (PAIR) {
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&tmem_base)) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+        } else {
+            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&tmem_base)) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        }
     }
     fence_before();
-    __syncthreads();
+    block_sync<PAIR>();
     fence_after();
     tad_wait_previous();
     const unsigned tmem = __shfl_sync(0xffffffffu, tmem_base, 0);
     constexpr unsigned SF = 256;                                          // first column of the scales
     bool ok = true;
 
-    if (warp == EPI_WARPS + SF_WARPS) {
+    if (warp >= EPI_WARPS) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REG_REST));
+    if (warp > EPI_WARPS + SF_WARPS + 1) {
+        // (the rest of the last warpgroup)
+    } else if (warp == EPI_WARPS + SF_WARPS) {
         // ---- copies ----
         int at = 0;
         unsigned long long issued = 0;
-        for (unsigned t = blockIdx.x; t < P.tiles && ok; t += gridDim.x) {
+        for (unsigned t = walker; t < P.tiles && ok; t += walkers) {
             int p0, q0, share;
-            tile_at(P, t, p0, q0, share, BN);
+            tile_at(P, t, p0, q0, share, TILE_P, BN);
             const int b1 = min(P.blocks, (share + 1) * P.each);
             for (int b = share * P.each; b < b1; ++b) {
                 const int turn = (int)(issued / S);
                 if (turn > 0 && !(ok = mbar_wait(empty + 8 * at, (turn - 1) & 1, &failed))) break;
                 if (lane == 0) {
                     const unsigned to = smem0 + at * C::STAGE, bar = full + 8 * at;
-                    mbar_expect(bar, C::STAGE);
-                    tma_load(to, &map_p, b * KB, p0, bar);
-                    tma_load(to + BM * KB, &map_q, b * KB, q0, bar);
+                    if (PAIR) {                        // the first block's barrier counts the bytes of both
+                        if (rank == 0) mbar_expect(bar, 2 * C::STAGE);
+                        const unsigned far = at_block(bar, 0), own = at_block(to, rank);
+                        tma_load_pair(own, &map_p, b * KB, p0 + (int)rank * BM, far);
+                        tma_load_pair(own + BM * KB, &map_q, b * KB, q0 + (int)rank * C::ROWS_Q, far);
+                    } else {
+                        mbar_expect(bar, C::STAGE);
+                        tma_load(to, &map_p, b * KB, p0, bar);
+                        tma_load(to + BM * KB, &map_q, b * KB, q0, bar);
+                    }
                 }
                 __syncwarp();
                 ++issued;
                 if (++at == S) at = 0;
             }
         }
-        // copies of a block that gave up still write its shared memory
-        if (!ok)
+        // copies of a block that gave up still write its shared memory (of a pair: the first block knows)
+        if (!ok && rank == 0)
             for (unsigned long long i = issued > S ? issued - S : 0; i < issued; ++i) mbar_drain(full + 8 * (unsigned)(i % S), (unsigned)(i / S) & 1);
     } else if (warp == EPI_WARPS + SF_WARPS + 1) {
         // ---- products ----
-        const unsigned base = (min((unsigned)BN, 256u) >> 3 << 17) | (1u << 23) | ((unsigned)(BM >> 4) << 24);
+        const unsigned base = ((unsigned)BN >> 3 << 17) | (1u << 23) | ((unsigned)(TILE_P >> 4) << 24);
         int at = 0, phase = 0, sf = 0, sf_phase = 0, n = 0;
-        for (unsigned t = blockIdx.x; t < P.tiles && ok; t += gridDim.x, ++n) {
+        for (unsigned t = walker; t < P.tiles && ok && rank == 0; t += walkers, ++n) {
             int p0, q0, share;
-            tile_at(P, t, p0, q0, share, BN);
+            tile_at(P, t, p0, q0, share, TILE_P, BN);
             const int b0 = share * P.each, b1 = min(P.blocks, b0 + P.each);
             if (n > 0) ok = mbar_wait(acc_empty, (n - 1) & 1, &failed);
             for (int b = b0; b < b1 && ok; ++b) {
@@ -199,105 +260,143 @@ tad_product8_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_cons
                 const unsigned idesc = base | ((unsigned)in << 4) | ((unsigned)in << 29);
                 const unsigned sfa = tmem + SF + sf * C::SF_COLS;
 #pragma unroll
-                for (int kk = 0; kk < KB / 32; ++kk) mma_scaled(tmem, da + 2 * kk, db + 2 * kk, idesc, sfa, sfa + 4, b > b0 || kk > 0);
-                mma_commit(empty + 8 * at);
+                for (int kk = 0; kk < KB / 32; ++kk) mma_scaled<PAIR>(tmem, da + 2 * kk, db + 2 * kk, idesc, sfa, sfa + 4, b > b0 || kk > 0);
+                mma_commit<PAIR>(empty + 8 * at);
                 if (++at == S) { at = 0; phase ^= 1; }
                 if (in == SF_BLOCKS - 1 || b + 1 == b1) {
-                    mma_commit(sf_empty + 8 * sf);
-                    if (++sf == 2) { sf = 0; sf_phase ^= 1; }
+                    mma_commit<PAIR>(sf_empty + 8 * sf);
+                    if (++sf == SF_BUFFERS) { sf = 0; sf_phase ^= 1; }
                 }
             }
-            if (ok) mma_commit(acc_full);
+            if (ok) mma_commit<PAIR>(acc_full);
         }
         // MMAs of a block that gave up still read its shared memory: all before this commit are done when it arrives (every other
         // role has left or leaves its waits, and nothing else arrives at this barrier)
-        if (!ok) {
-            mma_commit(acc_full);
+        if (!ok && rank == 0) {
+            mma_commit<PAIR>(acc_full);
             mbar_drain(acc_full, n & 1);
         }
     } else if (warp >= EPI_WARPS) {
-        // ---- scales: lane l of every quarter of tensor memory holds rows l, 32 + l, ... in columns 0, 1, ..., the scale of one block a byte ----
-        const int quad = warp & 3;
-        int sf = 0, turn = 0;
-        for (unsigned t = blockIdx.x; t < P.tiles && ok; t += gridDim.x) {
-            int p0, q0, share;
-            tile_at(P, t, p0, q0, share, BN);
-            const int b1 = min(P.blocks, (share + 1) * P.each);
-            for (int b = share * P.each; b < b1; b += SF_BLOCKS) {
-                unsigned w[1 + C::SF_Q / 4][4];
+        // ---- scales: lane l of every quarter of tensor memory holds rows l, 32 + l, ... in columns 0, 1, ..., the scale of one block a byte.
+        // A thread loads the words of one row of p and one or two of q, DEEP chunks ahead, and they are spread to the lanes through shared
+        // memory (loaded by every warp for itself they are 32 rows an instruction).  Eight buffers: the chain from memory to tensor memory is
+        // longer than the MMAs of a chunk, but never theirs to wait for ----
+        constexpr int ROWS = BM + (BN < 128 ? 128 : BN), OWN = ROWS / (SF_WARPS * 32), DEEP = 4;
+        const int quad = warp & 3, thread = threadIdx.x - EPI_WARPS * 32;
+        unsigned at_t = walker;                                    // the next chunk to be loaded
+        int p0 = 0, q0 = 0, b = 0, b1 = 0;
+        auto tile = [&] {
+            int share;
+            if (at_t >= P.tiles) return;
+            tile_at(P, at_t, p0, q0, share, TILE_P, BN);
+            b = share * P.each;
+            b1 = min(P.blocks, b + P.each);
+        };
+        unsigned mine[DEEP][OWN];
+        bool there[DEEP];
+        auto load = [&](unsigned (&w)[OWN]) {                      // false: there is no further chunk
+            if (at_t >= P.tiles) return false;
 #pragma unroll
-                for (int g = 0; g < 1 + C::SF_Q / 4; ++g)
+            for (int g = 0; g < OWN; ++g) {
+                const int in = thread + (g - 1) * 128;             // among the rows of q (g > 0)
+                const int64_t row = g == 0 ? p0 + (int)rank * BM + thread : q0 + in;
+                w[g] = 0x7f7f7f7fu;
+                if (row < (g == 0 ? P.np : P.nq) && (g == 0 || in < BN))
+                    w[g] = *reinterpret_cast<const unsigned *>(g == 0 ? P.sp + row * P.sps + b : P.sq + row * P.sqs + b);
+            }
+            b += SF_BLOCKS;
+            if (b >= b1) { at_t += walkers; tile(); }
+            return true;
+        };
+        tile();
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        const int64_t row = (g == 0 ? p0 : q0 + (g - 1) * 128) + c * 32 + lane;
-                        const bool live = row < (g == 0 ? P.np : P.nq) && (g == 0 || (g - 1) * 128 + c * 32 + lane < BN);
-                        w[g][c] = live ? *reinterpret_cast<const unsigned *>(g == 0 ? P.sp + row * P.sps + b : P.sq + row * P.sqs + b) : 0x7f7f7f7fu;
-                    }
-                if (turn > 1 && !(ok = mbar_wait(sf_empty + 8 * sf, ((turn >> 1) - 1) & 1, &failed))) break;
+        for (int d = 0; d < DEEP; ++d) there[d] = load(mine[d]);
+        for (int turn = 0; there[0]; ) {
+#pragma unroll
+            for (int d = 0; d < DEEP; ++d) {
+                if (!there[d]) { there[0] = false; break; }
+                unsigned *room = spread[d & 1];
+#pragma unroll
+                for (int g = 0; g < OWN; ++g) room[g * 128 + thread] = mine[d][g];
+                there[d] = load(mine[d]);
+                // (the room of two turns ago has been read by all four warps: they have met at the barrier of the turn between)
+                asm volatile("bar.sync 1, 128;" ::: "memory");
+                unsigned w[OWN][4];
+#pragma unroll
+                for (int g = 0; g < OWN; ++g)
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) w[g][c] = room[g * 128 + c * 32 + lane];
+                const int sf = turn % SF_BUFFERS;
+                if (turn >= SF_BUFFERS && ok) ok = mbar_wait(sf_empty + 8 * sf, (turn / SF_BUFFERS - 1) & 1, &failed);
+                ++turn;
+                if (!ok) continue;                                 // (all four warps stay in step at the barrier)
                 fence_after();
                 const unsigned to = tmem + ((unsigned)(quad * 32) << 16) + SF + sf * C::SF_COLS;
 #pragma unroll
-                for (int g = 0; g < 1 + C::SF_Q / 4; ++g) tmem_st4(to + 4 * g, w[g]);
+                for (int g = 0; g < OWN; ++g) tmem_st4(to + 4 * g, w[g]);
                 asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
                 fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(sf_full + 8 * sf);
-                sf ^= 1;
-                ++turn;
+                if (lane == 0) { if (PAIR) mbar_arrive_far(at_block(sf_full + 8 * sf, 0)); else mbar_arrive(sf_full + 8 * sf); }
             }
         }
     } else {
-        // ---- results: a warp empties a quarter of the lanes in half of the columns ----
-        constexpr int HALF = BN >= 64 ? BN / 2 : BN, COLS = HALF < 32 ? 32 : HALF;          // columns that a warp reads, 32 at a time
+        // ---- results: a warp empties a quarter of the lanes in half of the columns, all of them into registers before the first is stored, so
+        // that the next tile's MMAs wait for that alone (there is room for one accumulator of 256 columns beside the scales) ----
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REG_EPI));
+        constexpr int HALF = BN >= 64 ? BN / 2 : 32;                                       // columns that a warp reads
         const int quad = warp & 3, half = BN >= 64 ? warp >> 2 : 0;
         const bool idle = BN < 64 && warp >= 4;
         int n = 0;
-        for (unsigned t = blockIdx.x; t < P.tiles; t += gridDim.x, ++n) {
+        for (unsigned t = walker; t < P.tiles; t += walkers, ++n) {
             int p0, q0, share;
-            tile_at(P, t, p0, q0, share, BN);
+            tile_at(P, t, p0, q0, share, TILE_P, BN);
             ok = ok && mbar_wait(acc_full, n & 1, &failed);
             fence_after();
-            const int p = p0 + quad * 32 + lane;
-            const int live = p < P.np && !idle ? min(HALF, P.nq - q0 - half * HALF) : 0;       // columns of this thread
-            const unsigned from = tmem + ((unsigned)(quad * 32) << 16) + half * HALF;
-            const int64_t o = P.plane * share + p * P.yp + (int64_t)(q0 + half * HALF) * P.yq;
-            auto put = [&](auto *out, int c, const float (&v)[32]) {                        // columns c .. c + 31
-                using T = typename std::remove_pointer<decltype(out)>::type;
-                T *to = out + o + c * P.yq;
-                if (P.vec && c + 32 <= live) {
+            float v[HALF];
+            if (ok && !idle) {
+                const unsigned from = tmem + ((unsigned)(quad * 32) << 16) + half * HALF;
 #pragma unroll
-                    for (int j = 0; j < 32; j += 8) {
-                        Piece<T, 8> x;
-                        const float e[8] = {v[j], v[j + 1], v[j + 2], v[j + 3], v[j + 4], v[j + 5], v[j + 6], v[j + 7]};
-                        x.set(e);
-                        x.store(to + j);
-                    }
-                } else {
+                for (int c = 0; c < HALF; c += 32) tmem_ld32(from + c, *reinterpret_cast<float (*)[32]>(&v[c]));
+                tmem_wait_ld();
+            } else {
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) if (c + j < live) to[j * P.yq] = from_float<T>(v[j]);
-                }
-            };
-            const float nan = __uint_as_float(0x7fffffffu);
-            if (!idle) {
-#pragma unroll
-                for (int c = 0; c < COLS; c += 32) {
-                    float v[32];
-                    if (ok) tmem_ld32(from + c, v);
-                    else for (int j = 0; j < 32; ++j) v[j] = nan;               // a wait ran out: nothing that looks like a result
-                    if (P.type == TAD_F32) put(static_cast<float *>(P.y), c, v);
-                    else if (P.type == TAD_BF16) put(static_cast<__nv_bfloat16 *>(P.y), c, v);
-                    else put(static_cast<__half *>(P.y), c, v);
-                }
+                for (int j = 0; j < HALF; ++j) v[j] = __uint_as_float(0x7fffffffu);         // a wait ran out: nothing that looks like a result
             }
             fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(acc_empty);
+            if (lane == 0) { if (PAIR) mbar_arrive_far(at_block(acc_empty, 0)); else mbar_arrive(acc_empty); }
+            const int p = p0 + (int)rank * BM + quad * 32 + lane;
+            const int live = p < P.np && !idle ? min(HALF, P.nq - q0 - half * HALF) : 0;       // columns of this thread
+            const int64_t o = P.plane * share + p * P.yp + (int64_t)(q0 + half * HALF) * P.yq;
+            auto put = [&](auto *out) {
+                using T = typename std::remove_pointer<decltype(out)>::type;
+                T *to = out + o;
+                if (P.vec && live == HALF) {
+#pragma unroll
+                    for (int j = 0; j < HALF; j += 32 / (int)sizeof(T)) {                     // 32 bytes: whole sectors
+                        unsigned w[8];
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) w[k] = word_of<T>(&v[j + k * (4 / (int)sizeof(T))]);
+                        asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(to + j), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
+                    }
+                } else {
+#pragma unroll
+                    for (int j = 0; j < HALF; ++j) if (j < live) to[j * P.yq] = from_float<T>(v[j]);
+                }
+            };
+            if (P.type == TAD_F32) put(static_cast<float *>(P.y));
+            else if (P.type == TAD_BF16) put(static_cast<__nv_bfloat16 *>(P.y));
+            else put(static_cast<__half *>(P.y));
         }
     }
     fence_before();
-    __syncthreads();
+    block_sync<PAIR>();
     fence_after();
-    if (warp == EPI_WARPS) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+    if (warp == EPI_WARPS) {
+        if (PAIR) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+        else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+    }
 }
 
 // ---- few rows ----
@@ -404,7 +503,7 @@ tad_product8_zero_kernel(int64_t m, int n, void *y, int64_t ys, int type)
 
 // how a product is run: the longer side is p where the other one fits into one tile
 struct Way {
-    bool few, p_is_b;
+    bool few, p_is_b, pair;
     int bn, split, each, blocks;
     int64_t tiles_p, tiles_q;
 };
@@ -426,10 +525,14 @@ Way way_of(int64_t m, int64_t n, int64_t k)
         const double t256 = (double)((tiles(256) + SMS - 1) / SMS), t128 = 0.55 * (double)((tiles(128) + SMS - 1) / SMS);
         w.bn = nq > 128 && t256 <= t128 ? 256 : 128;
     }
+    // pairs where they have work for all SMs
+    const int64_t pairs = ((np + 2 * BM - 1) / (2 * BM)) * ((nq + 255) / 256);
+    w.pair = nq > 128 && pairs >= SMS / 2;
+    if (w.pair) { w.bn = 256; w.tiles_p = (np + 2 * BM - 1) / (2 * BM); }
     w.tiles_q = (nq + w.bn - 1) / w.bn;
     // fewer tiles than SMs: k in shares of whole words of scales
     const int64_t t = w.tiles_p * w.tiles_q;
-    int64_t split = t < SMS ? std::min<int64_t>(SMS / t, (w.blocks + 2 * SF_BLOCKS - 1) / (2 * SF_BLOCKS)) : 1;
+    int64_t split = t < SMS && !w.pair ? std::min<int64_t>(SMS / t, (w.blocks + 2 * SF_BLOCKS - 1) / (2 * SF_BLOCKS)) : 1;
     split = std::max<int64_t>(1, split);
     w.each = (int)((w.blocks + split - 1) / split);
     w.each = (w.each + SF_BLOCKS - 1) / SF_BLOCKS * SF_BLOCKS;
@@ -461,7 +564,7 @@ bool map_of(CUtensorMap *map, const tad_packed *m, int64_t rows, int64_t k, int 
                   CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int BN>
+template <int BN, bool PAIR>
 cudaError_t launch_product(const CUtensorMap &mp, const CUtensorMap &mq, const Product &P, cudaStream_t stream)
 {
     static std::atomic<bool> allowed[64];
@@ -469,11 +572,17 @@ cudaError_t launch_product(const CUtensorMap &mp, const CUtensorMap &mq, const P
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
     if (dev < 0 || dev >= 64 || !allowed[dev].load(std::memory_order_relaxed)) {
-        e = cudaFuncSetAttribute(tad_product8_kernel<BN>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Config<BN>::SMEM);
+        e = cudaFuncSetAttribute(tad_product8_kernel<BN, PAIR>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Config<BN, PAIR>::SMEM);
         if (e != cudaSuccess) return e;
+        // the warpgroups' register shares must fit into what the block is launched with
+        cudaFuncAttributes at;
+        e = cudaFuncGetAttributes(&at, tad_product8_kernel<BN, PAIR>);
+        if (e != cudaSuccess) return e;
+        if (at.numRegs * NT < EPI_WARPS * 32 * REG_EPI + (NT - EPI_WARPS * 32) * REG_REST) return cudaErrorInvalidConfiguration;
         if (dev >= 0 && dev < 64) allowed[dev].store(true, std::memory_order_relaxed);
     }
-    return tad_launch(tad_product8_kernel<BN>, std::min(P.tiles, (unsigned)SMS), NT, Config<BN>::SMEM, stream, mp, mq, P);
+    if (PAIR) return tad_launch_cluster(tad_product8_kernel<BN, PAIR>, 2 * std::min(P.tiles, (unsigned)SMS / 2), NT, Config<BN, PAIR>::SMEM, stream, 2, mp, mq, P);
+    return tad_launch(tad_product8_kernel<BN, PAIR>, std::min(P.tiles, (unsigned)SMS), NT, Config<BN, PAIR>::SMEM, stream, mp, mq, P);
 }
 
 }  // namespace
@@ -526,10 +635,11 @@ tad_status tad_matmul8(const tad_packed *a, const tad_packed *b, int64_t m, int6
     P.y = y->data; P.type = y->type;
     if (w.split > 1) { P.y = workspace; P.type = TAD_F32; P.plane = elements; stride = n; }
     P.yp = w.p_is_b ? 1 : stride; P.yq = w.p_is_b ? stride : 1;
-    P.vec = !w.p_is_b && reinterpret_cast<uintptr_t>(P.y) % 16 == 0 && (stride * (int64_t)type_size(P.type)) % 16 == 0 && (P.plane * 4) % 16 == 0;
+    P.vec = !w.p_is_b && reinterpret_cast<uintptr_t>(P.y) % 32 == 0 && stride * (int64_t)type_size(P.type) % 32 == 0 && P.plane % 8 == 0;
     CUtensorMap mp, mq;
-    if (!map_of(&mp, p, P.np, k, BM) || !map_of(&mq, q, P.nq, k, w.bn)) { tad::set_error("matmul8: no tensor map for this matrix (or no driver)"); return TAD_ERR_CUDA; }
-    e = w.bn == 256 ? launch_product<256>(mp, mq, P, stream) : w.bn == 128 ? launch_product<128>(mp, mq, P, stream) : w.bn == 64 ? launch_product<64>(mp, mq, P, stream) : launch_product<32>(mp, mq, P, stream);
+    if (!map_of(&mp, p, P.np, k, BM) || !map_of(&mq, q, P.nq, k, w.pair ? w.bn / 2 : w.bn)) { tad::set_error("matmul8: no tensor map for this matrix (or no driver)"); return TAD_ERR_CUDA; }
+    e = w.pair ? launch_product<256, true>(mp, mq, P, stream) : w.bn == 256 ? launch_product<256, false>(mp, mq, P, stream) : w.bn == 128 ? launch_product<128, false>(mp, mq, P, stream) :
+        w.bn == 64 ? launch_product<64, false>(mp, mq, P, stream) : launch_product<32, false>(mp, mq, P, stream);
     if (e == cudaSuccess && w.split > 1)
         e = tad_launch(tad_product8_planes_kernel, (unsigned)((elements + 255) / 256), 256, 0, stream, static_cast<const float *>(workspace), w.split, m, (int)n, y->data, y->stride, (int)y->type);
     return launched("product", e);
