@@ -40,13 +40,15 @@ __device__ __forceinline__ unsigned at_block(unsigned bar, unsigned rank)
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(bar), "r"(rank));
     return r;
 }
-__device__ __forceinline__ void mbar_arrive_far(unsigned bar) { asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory"); }
+// Relaxed: what the blocks of a pair tell each other so lies in tensor memory (written or read by completed instructions, in front of the fence
+// for them).  A release would wait for every earlier access of the thread: 2 us for the scales of a chunk, whose MMAs take 1.
+__device__ __forceinline__ void mbar_arrive_far(unsigned bar) { asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory"); }
 __device__ __forceinline__ void mbar_arrive(unsigned bar) { asm volatile("{ .reg .b64 t; mbarrier.arrive.shared::cta.b64 t, [%0]; }" ::"r"(bar) : "memory"); }
 __device__ __forceinline__ void mbar_expect(unsigned bar, unsigned bytes) { asm volatile("{ .reg .b64 t; mbarrier.arrive.expect_tx.shared::cta.b64 t, [%0], %1; }" ::"r"(bar), "r"(bytes) : "memory"); }
 __device__ __forceinline__ bool mbar_try(unsigned bar, unsigned parity)
 {
     unsigned ok;
-    asm volatile("{ .reg .pred p; mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    asm volatile("{ .reg .pred p; mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
     return ok != 0;
 }
 // (by whole warps) false: this wait ran out, or another one of the block did
