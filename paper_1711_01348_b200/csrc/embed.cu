@@ -36,8 +36,8 @@ struct Tokens {
 
 constexpr int NT = 256, ROWS = 4;
 
-// ROWS rows of V elements a thread; 2^log threads stand beside each other in a row
-template <class S, class T, int V>
+// ROWS rows of eight elements a thread; 2^log threads stand beside each other in a row
+template <class S, class T>
 __global__ void __launch_bounds__(NT)
 tad_embed_forward_kernel(const Tokens tok, int64_t n, const S *__restrict__ table, int64_t ts, int width, float factor, T *__restrict__ y,
                          int64_t ys, int log, unsigned chunks)
@@ -46,12 +46,12 @@ tad_embed_forward_kernel(const Tokens tok, int64_t n, const S *__restrict__ tabl
     const unsigned group = blockIdx.x / chunks, chunk = blockIdx.x - group * chunks;
     const int step = NT >> log;
     const int64_t t0 = (int64_t)group * (ROWS * step) + (threadIdx.x >> log);
-    const int64_t c = ((int64_t)(chunk << log) + (threadIdx.x & ((1 << log) - 1))) * V;
+    const int64_t c = ((int64_t)(chunk << log) + (threadIdx.x & ((1 << log) - 1))) * 8;
     if (c >= width) return;
     unsigned key[ROWS];
 #pragma unroll
     for (int i = 0; i < ROWS; ++i) key[i] = t0 + i * step < n ? tok.key(t0 + i * step) : tok.n_table;
-    Piece<S, V> p[ROWS];
+    Piece<S, 8> p[ROWS];
 #pragma unroll
     for (int i = 0; i < ROWS; ++i) {
         p[i].zero();
@@ -60,14 +60,37 @@ tad_embed_forward_kernel(const Tokens tok, int64_t n, const S *__restrict__ tabl
 #pragma unroll
     for (int i = 0; i < ROWS; ++i) {
         if (t0 + i * step >= n) continue;
-        float v[V];
+        float v[8];
         p[i].get(v);
 #pragma unroll
-        for (int j = 0; j < V; ++j) v[j] = key[i] < tok.n_table ? v[j] * factor : 0.f;      // (zeros even where the factor is not finite)
-        Piece<T, V> o;
+        for (int j = 0; j < 8; ++j) v[j] = key[i] < tok.n_table ? v[j] * factor : 0.f;      // (zeros even where the factor is not finite)
+        Piece<T, 8> o;
         o.set(v);
         o.store(y + (t0 + i * step) * ys + c);
     }
+}
+
+// Rows off 16-byte boundaries: a warp a row and 512 columns, sixteen elements a lane, 32 apart, so that every access is the lane's pointer and
+// a constant (one element a thread and row: 16384 rows of 1001 bf16 35 us for 15)
+constexpr int ODD = 16;
+template <class S, class T>
+__global__ void __launch_bounds__(NT)
+tad_embed_forward_odd_kernel(const Tokens tok, int64_t n, const S *__restrict__ table, int64_t ts, int width, float factor, T *__restrict__ y,
+                             int64_t ys, unsigned chunks)
+{
+    tad_wait_previous();
+    const int64_t unit = (int64_t)blockIdx.x * (NT / 32) + (threadIdx.x >> 5), t = unit / chunks;
+    if (t >= n) return;
+    const int c = (int)(unit - t * chunks) * (32 * ODD) + (threadIdx.x & 31), rem = width - c;
+    const unsigned key = tok.key(t);
+    const bool inside = key < tok.n_table;
+    const S *__restrict__ from = table + (inside ? (int64_t)key * ts : 0) + c;
+    T *__restrict__ to = y + t * ys + c;
+    S v[ODD];
+#pragma unroll
+    for (int i = 0; i < ODD; ++i) if (inside && 32 * i < rem) v[i] = from[32 * i];
+#pragma unroll
+    for (int i = 0; i < ODD; ++i) if (32 * i < rem) to[32 * i] = from_float<T>(inside ? to_float(v[i]) * factor : 0.f);
 }
 
 // ---- the sort ----
@@ -170,7 +193,7 @@ constexpr int CLEAR_NT = 1024;
 constexpr unsigned MAP_ROWS = 32768;                           // rows whose use is noted at a time, a bit each
 
 __global__ void __launch_bounds__(CLEAR_NT)
-tad_embed_clear_kernel(const Tokens tok, const unsigned n, const int64_t each, unsigned char *dtable, const int64_t stride, const int64_t row_bytes, const int piece,
+tad_embed_clear_kernel(const Tokens tok, const unsigned n, const int64_t each, unsigned char *dtable, const int64_t stride, const int64_t row_bytes,
                        const bool beside)
 {
     __shared__ unsigned map[MAP_ROWS / 32];
@@ -194,13 +217,12 @@ tad_embed_clear_kernel(const Tokens tok, const unsigned n, const int64_t each, u
         for (unsigned i = warp; i < rows; i += CLEAR_NT / 32) {
             if (map[i >> 5] >> (i & 31) & 1) continue;
             unsigned char *to = dtable + (r0 + i) * stride;
-            if (piece == 32)
-                for (int64_t b = lane * 32; b < row_bytes; b += 1024)
-                    asm volatile("st.global.v8.b32 [%0], {%1,%1,%1,%1,%1,%1,%1,%1};" ::"l"(to + b), "r"(0) : "memory");
-            else if (piece == 4)
-                for (int64_t b = lane * 4; b < row_bytes; b += 128) *reinterpret_cast<unsigned *>(to + b) = 0;
-            else
-                for (int64_t b = lane * 2; b < row_bytes; b += 64) *reinterpret_cast<unsigned short *>(to + b) = 0;
+            // whole sectors from the row's first boundary of 32 bytes on, two bytes a lane before and behind them
+            const int64_t head = min(row_bytes, (int64_t)(-reinterpret_cast<uintptr_t>(to) & 31)), body = (row_bytes - head) & ~int64_t(31);
+            if (lane * 2 < head) *reinterpret_cast<unsigned short *>(to + lane * 2) = 0;
+            for (int64_t b = head + lane * 32; b < head + body; b += 1024)
+                asm volatile("st.global.v8.b32 [%0], {%1,%1,%1,%1,%1,%1,%1,%1};" ::"l"(to + b), "r"(0) : "memory");
+            if (lane * 2 < row_bytes - head - body) *reinterpret_cast<unsigned short *>(to + head + body + lane * 2) = 0;
         }
     }
     if (beside) tad_wait_previous();
@@ -474,13 +496,19 @@ template <class S, class T>
 cudaError_t embed_forward(const Tokens &tok, int64_t n, const tad_rows *table, int64_t width, float factor, const tad_rows *y, cudaStream_t stream)
 {
     const bool eights = width % 8 == 0 && by_eights(table) && by_eights(y);
-    const int64_t pieces = eights ? width / 8 : width;
+    if (!eights) {
+        const int64_t chunks = (width + 32 * ODD - 1) / (32 * ODD), blocks = (n * chunks + NT / 32 - 1) / (NT / 32);
+        if (blocks >= MAX_ROWS) return cudaErrorInvalidValue;
+        return tad_launch(tad_embed_forward_odd_kernel<S, T>, (unsigned)blocks, NT, 0, stream, tok, n, static_cast<const S *>(table->data), table->stride, (int)width, factor,
+                          static_cast<T *>(y->data), y->stride, (unsigned)chunks);
+    }
+    const int64_t pieces = width / 8;
     int log = 0;
     while (log < 8 && (int64_t(1) << log) < pieces) ++log;
     const int64_t chunks = (pieces + (1 << log) - 1) >> log, rows = ROWS * (NT >> log), blocks = (n + rows - 1) / rows * chunks;
     if (blocks >= MAX_ROWS) return cudaErrorInvalidValue;
-    return tad_launch(eights ? tad_embed_forward_kernel<S, T, 8> : tad_embed_forward_kernel<S, T, 1>, (unsigned)blocks, NT, 0, stream, tok, n,
-                      static_cast<const S *>(table->data), table->stride, (int)width, factor, static_cast<T *>(y->data), y->stride, log, (unsigned)chunks);
+    return tad_launch(tad_embed_forward_kernel<S, T>, (unsigned)blocks, NT, 0, stream, tok, n, static_cast<const S *>(table->data), table->stride, (int)width, factor,
+                      static_cast<T *>(y->data), y->stride, log, (unsigned)chunks);
 }
 
 }  // namespace
@@ -543,10 +571,9 @@ tad_status tad_embed_backward(const void *tokens, int32_t token_bits, int64_t n_
     }
     if (!accumulate) {
         const int64_t size = (int64_t)type_size(dtable->type), stride = dtable->stride * size, row_bytes = width * size;
-        auto whole = [&](int64_t b) { return reinterpret_cast<uintptr_t>(dtable->data) % b == 0 && stride % b == 0 && row_bytes % b == 0; };
         const int64_t blocks = std::min<int64_t>(SMS, (n_table + 31) / 32), each = (n_table + blocks - 1) / blocks;
         e = tad_launch(tad_embed_clear_kernel, (unsigned)blocks, CLEAR_NT, 0, stream, tok, (unsigned)n_tokens, each, static_cast<unsigned char *>(dtable->data), stride,
-                       row_bytes, whole(32) ? 32 : whole(4) ? 4 : 2, n_tokens > 0);
+                       row_bytes, n_tokens > 0);
         if (e != cudaSuccess || n_tokens == 0) return launched("clearing of rows without tokens", e);
     }
     Sums P{};

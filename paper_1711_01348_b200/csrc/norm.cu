@@ -533,21 +533,27 @@ struct HeldSource {
 };
 template <int E>
 struct HeldSource<Packed8, E> {
-    Source<Packed8, 1> p[E];
+    uint8_t q[E], s[(E + 3) / 4];          // (four elements of a thread, 32 apart, lie in one block of 128: its first column is a multiple of 256)
     __device__ __forceinline__ void zero()
     {
 #pragma unroll
-        for (int i = 0; i < E; ++i) p[i].zero();
+        for (int i = 0; i < E; ++i) q[i] = 0;
+#pragma unroll
+        for (int k = 0; k < (E + 3) / 4; ++k) s[k] = 127;
     }
     __device__ __forceinline__ void fetch(const Params &P, int64_t r, int col, int rem)
     {
+        const uint8_t *from = P.q + r * P.qs + col, *scale = P.scale + r * P.ss + col / TAD_BLOCK8;
 #pragma unroll
-        for (int i = 0; i < E; ++i) if (Of<1>::place(i) < rem) p[i].load(P, r, col + Of<1>::place(i));
+        for (int i = 0; i < E; ++i) if (Of<1>::place(i) < rem) q[i] = from[Of<1>::place(i)];
+#pragma unroll
+        for (int k = 0; k < (E + 3) / 4; ++k) if (Of<1>::place(4 * k) < rem) s[k] = scale[k];
     }
     __device__ __forceinline__ void get(float (&v)[E]) const
     {
+        static_assert(E == 1 || E % 4 == 0, "whole blocks");
 #pragma unroll
-        for (int i = 0; i < E; ++i) { float f[1]; p[i].get(f); v[i] = f[0]; }
+        for (int i = 0; i < E; ++i) v[i] = from_e4m3x2(q[i]).x * scale_of(s[i / 4]);
     }
 };
 

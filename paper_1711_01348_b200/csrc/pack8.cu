@@ -14,9 +14,9 @@ using namespace tadr;
 constexpr int NT = 256, ROWS = 4;          // threads of a block; rows that a thread has under way
 
 // A block of 128 belongs to 2^own neighbouring threads: to pack, eight (sixteen elements each); to unpack, sixteen, because a thread's store
-// is one piece of 16 bytes then (two of them, 32 bytes apart in a warp: 81 % of the memory rate for 97 %); off 16-byte boundaries a
-// warp, whose lanes take every 32nd element.  A thread block covers 2^cb blocks of a row (all that its threads own or, in narrow
-// matrices, the whole row), and ROWS times as many rows as that leaves it threads for.
+// is one piece of 16 bytes then (two of them, 32 bytes apart in a warp: 81 % of the memory rate for 97 %).  A thread block covers 2^cb
+// blocks of a row (all that its threads own or, in narrow matrices, the whole row), and ROWS times as many rows as that leaves it
+// threads for.
 struct Cover {
     int64_t row0;            // first row of this thread, the next ones are `step` rows on
     int step, blk, in;       // its block of 128 in the row, its place among the block's threads
@@ -30,7 +30,7 @@ struct Cover {
         in = threadIdx.x & ((1 << own) - 1);
     }
 };
-constexpr int OWN_PACK = 3, OWN_UNPACK = 4, OWN_ODD = 5;
+constexpr int OWN_PACK = 3, OWN_UNPACK = 4;
 
 template <class T>
 __global__ void __launch_bounds__(NT)
@@ -101,69 +101,72 @@ tad_unpack8_kernel(const uint8_t *__restrict__ q, int64_t qs, const uint8_t *__r
     }
 }
 
-// rows of x off 16-byte boundaries
+// Rows of x off 16-byte boundaries: a warp a row and ODD blocks of 128, four elements of each a lane, 32 apart, so that every access is
+// the lane's pointer and a constant.
+constexpr int ODD = 4;
+
 template <class T>
 __global__ void __launch_bounds__(NT)
-tad_pack8_odd_kernel(const T *__restrict__ x, int64_t xs, int64_t n_rows, int width, int cb, unsigned chunks,
+tad_pack8_odd_kernel(const T *__restrict__ x, int64_t xs, int64_t n_rows, int width, unsigned chunks,
                      uint8_t *__restrict__ q, int64_t qs, uint8_t *__restrict__ scale, int64_t ss)
 {
     tad_wait_previous();
-    const Cover at(OWN_ODD, cb, chunks);
-    const int col = at.blk * TAD_BLOCK8 + at.in;
-    T raw[ROWS][4];
+    const int64_t unit = (int64_t)blockIdx.x * (NT / 32) + (threadIdx.x >> 5), r = unit / chunks;
+    if (r >= n_rows) return;
+    const int lane = threadIdx.x & 31, c = (int)(unit - r * chunks) * (ODD * TAD_BLOCK8) + lane, rem = width - c;
+    const T *__restrict__ from = x + r * xs + c;
+    uint8_t *__restrict__ to = q + r * qs + c;
+    T raw[4 * ODD];
 #pragma unroll
-    for (int i = 0; i < ROWS; ++i) {
-        const int64_t r = at.row0 + i * at.step;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            raw[i][j] = from_float<T>(0.f);
-            if (r < n_rows && col + 32 * j < width) raw[i][j] = x[r * xs + col + 32 * j];
-        }
+    for (int i = 0; i < 4 * ODD; ++i) {
+        raw[i] = from_float<T>(0.f);
+        if (32 * i < rem) raw[i] = from[32 * i];
     }
 #pragma unroll
-    for (int i = 0; i < ROWS; ++i) {
-        const int64_t r = at.row0 + i * at.step;
+    for (int k = 0; k < ODD; ++k) {
         float v[4], a = 0.f;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) { v[j] = to_float(raw[i][j]); a = fmaxf(a, finite_abs(v[j])); }
+        for (int j = 0; j < 4; ++j) { v[j] = to_float(raw[4 * k + j]); a = fmaxf(a, finite_abs(v[j])); }
 #pragma unroll
         for (int d = 16; d; d >>= 1) a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, d));
-        if (r >= n_rows) continue;
         const unsigned s = scale_byte(a);
         const float inv = inverse_scale(s);
+        const unsigned lo = to_e4m3x2(no_infinity(v[0]) * inv, no_infinity(v[1]) * inv), hi = to_e4m3x2(no_infinity(v[2]) * inv, no_infinity(v[3]) * inv);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) if (col + 32 * j < width) q[r * qs + col + 32 * j] = (uint8_t)to_e4m3x2(no_infinity(v[j]) * inv, 0.f);
-        if (at.in == 0 && col < width) scale[r * ss + at.blk] = (uint8_t)s;
+        for (int j = 0; j < 4; ++j) if (32 * (4 * k + j) < rem) to[32 * (4 * k + j)] = (uint8_t)((j < 2 ? lo : hi) >> (8 * (j & 1)));
+        if (lane == 0 && 128 * k < rem) scale[r * ss + c / TAD_BLOCK8 + k] = (uint8_t)s;
     }
 }
 
 template <class T>
 __global__ void __launch_bounds__(NT)
 tad_unpack8_odd_kernel(const uint8_t *__restrict__ q, int64_t qs, const uint8_t *__restrict__ scale, int64_t ss, int64_t n_rows, int width,
-                       int cb, unsigned chunks, T *__restrict__ x, int64_t xs)
+                       unsigned chunks, T *__restrict__ x, int64_t xs)
 {
     tad_wait_previous();
-    const Cover at(OWN_ODD, cb, chunks);
-    const int col = at.blk * TAD_BLOCK8 + at.in;
-    uint8_t p[ROWS][4];
-    unsigned s[ROWS];
+    const int64_t unit = (int64_t)blockIdx.x * (NT / 32) + (threadIdx.x >> 5), r = unit / chunks;
+    if (r >= n_rows) return;
+    const int lane = threadIdx.x & 31, c = (int)(unit - r * chunks) * (ODD * TAD_BLOCK8) + lane, rem = width - c;
+    const uint8_t *__restrict__ from = q + r * qs + c;
+    T *__restrict__ to = x + r * xs + c;
+    uint8_t p[4 * ODD], s[ODD];
 #pragma unroll
-    for (int i = 0; i < ROWS; ++i) {
-        const int64_t r = at.row0 + i * at.step;
-        s[i] = 127;
-        if (r < n_rows && col < width) s[i] = scale[r * ss + at.blk];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            p[i][j] = 0;
-            if (r < n_rows && col + 32 * j < width) p[i][j] = q[r * qs + col + 32 * j];
-        }
+    for (int k = 0; k < ODD; ++k) {
+        s[k] = 127;
+        if (128 * k < rem + lane) s[k] = scale[r * ss + c / TAD_BLOCK8 + k];         // (the block exists: its first column is c - lane + 128 k)
     }
 #pragma unroll
-    for (int i = 0; i < ROWS; ++i) {
-        const int64_t r = at.row0 + i * at.step;
-        const float f = scale_of(s[i]);
+    for (int i = 0; i < 4 * ODD; ++i) {
+        p[i] = 0;
+        if (32 * i < rem) p[i] = from[32 * i];
+    }
 #pragma unroll
-        for (int j = 0; j < 4; ++j) if (r < n_rows && col + 32 * j < width) x[r * xs + col + 32 * j] = from_float<T>(from_e4m3x2(p[i][j]).x * f);
+    for (int k = 0; k < ODD; ++k) {
+        const float f = scale_of(s[k]);
+        const float2 lo = from_e4m3x2(p[4 * k] | (unsigned)p[4 * k + 1] << 8), hi = from_e4m3x2(p[4 * k + 2] | (unsigned)p[4 * k + 3] << 8);
+        const float v[4] = {lo.x * f, lo.y * f, hi.x * f, hi.y * f};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) if (32 * (4 * k + j) < rem) to[32 * (4 * k + j)] = from_float<T>(v[j]);
     }
 }
 
@@ -294,17 +297,33 @@ Launch cover(int64_t n_rows, int64_t n_blocks, int own)
     return l;
 }
 
+// a warp a row and ODD blocks of 128
+bool odd_cover(int64_t n_rows, int64_t width, unsigned &blocks, unsigned &chunks)
+{
+    const int64_t c = (width + ODD * TAD_BLOCK8 - 1) / (ODD * TAD_BLOCK8), b = (n_rows * c + NT / 32 - 1) / (NT / 32);
+    blocks = (unsigned)b;
+    chunks = (unsigned)c;
+    return b < MAX_ROWS;
+}
+
 }  // namespace
 
 // also called by the layer norm for a checkpoint that its own pass cannot write
 tad_status tad_launch_pack8(const tad_rows *x, int64_t n_rows, int64_t width, const tad_packed *out, cudaStream_t stream)
 {
-    const bool eights = by_eights(x);
-    const Launch l = cover(n_rows, tadr::blocks_of(width), eights ? OWN_PACK : OWN_ODD);
     cudaError_t e = cudaSuccess;
-    TAD_WITH_TYPE(x->type, T,
-        e = tad_launch(eights ? tad_pack8_kernel<T> : tad_pack8_odd_kernel<T>, l.blocks, NT, 0, stream, static_cast<const T *>(x->data), x->stride, n_rows, (int)width,
-                       l.cb, l.chunks, out->q, out->q_stride, out->scale, out->scale_stride));
+    if (by_eights(x)) {
+        const Launch l = cover(n_rows, tadr::blocks_of(width), OWN_PACK);
+        TAD_WITH_TYPE(x->type, T,
+            e = tad_launch(tad_pack8_kernel<T>, l.blocks, NT, 0, stream, static_cast<const T *>(x->data), x->stride, n_rows, (int)width, l.cb, l.chunks, out->q,
+                           out->q_stride, out->scale, out->scale_stride));
+    } else {
+        unsigned blocks = 0, chunks = 0;
+        if (!odd_cover(n_rows, width, blocks, chunks)) { tad::set_error("pack8: too many blocks"); return TAD_ERR_UNSUPPORTED; }
+        TAD_WITH_TYPE(x->type, T,
+            e = tad_launch(tad_pack8_odd_kernel<T>, blocks, NT, 0, stream, static_cast<const T *>(x->data), x->stride, n_rows, (int)width, chunks, out->q,
+                           out->q_stride, out->scale, out->scale_stride));
+    }
     return launched("pack", e);
 }
 
@@ -323,12 +342,20 @@ tad_status tad_unpack8(const tad_packed *in, int64_t n_rows, int64_t width, cons
     tad_status st;
     if ((st = check_sizes("unpack8", n_rows, width)) || (st = check_packed("unpack8: in", in, n_rows, width)) || (st = check_rows("unpack8: x", x, n_rows, width))) return st;
     if (n_rows == 0 || width == 0) return TAD_OK;
-    const bool eights = by_eights(x);
-    const Launch l = cover(n_rows, blocks_of(width), eights ? OWN_UNPACK : OWN_ODD);
+    const cudaStream_t stream = (cudaStream_t)cuda_stream;
     cudaError_t e = cudaSuccess;
-    TAD_WITH_TYPE(x->type, T,
-        e = tad_launch(eights ? tad_unpack8_kernel<T> : tad_unpack8_odd_kernel<T>, l.blocks, NT, 0, (cudaStream_t)cuda_stream, in->q, in->q_stride, in->scale, in->scale_stride,
-                       n_rows, (int)width, l.cb, l.chunks, static_cast<T *>(x->data), x->stride));
+    if (by_eights(x)) {
+        const Launch l = cover(n_rows, blocks_of(width), OWN_UNPACK);
+        TAD_WITH_TYPE(x->type, T,
+            e = tad_launch(tad_unpack8_kernel<T>, l.blocks, NT, 0, stream, in->q, in->q_stride, in->scale, in->scale_stride, n_rows, (int)width, l.cb, l.chunks,
+                           static_cast<T *>(x->data), x->stride));
+    } else {
+        unsigned blocks = 0, chunks = 0;
+        if (!odd_cover(n_rows, width, blocks, chunks)) { tad::set_error("unpack8: too many blocks"); return TAD_ERR_UNSUPPORTED; }
+        TAD_WITH_TYPE(x->type, T,
+            e = tad_launch(tad_unpack8_odd_kernel<T>, blocks, NT, 0, stream, in->q, in->q_stride, in->scale, in->scale_stride, n_rows, (int)width, chunks,
+                           static_cast<T *>(x->data), x->stride));
+    }
     return launched("unpack", e);
 }
 
