@@ -390,7 +390,7 @@ tad_embed_sums_kernel(const Sums P)
 }
 
 // The token that ends in segment s and began in an earlier one is the sum of the tails from there on and the head of s.  A warp a segment
-// and slice; where there are many tails, the warps of the block share them.
+// and slice; where there are many tails, the warps of the block share them (the slices of a segment lie in different blocks then).
 constexpr unsigned MANY = 16;
 
 template <int V>
@@ -415,8 +415,8 @@ tad_embed_join_kernel(const Sums P)
             for (int e = 0; e < 8; ++e) a[e] += v[e];
         }
     };
-    const unsigned unit0 = blockIdx.x * WARPS, unit = unit0 + warp, s = unit / P.slices, slice = unit - s * P.slices;
-    const Cut cut = s < P.segments ? P.cuts[s] : Cut{0, 0};
+    const unsigned unit0 = blockIdx.x * WARPS, unit = unit0 + warp, slice = unit / P.segments, s = unit - slice * P.segments;
+    const Cut cut = slice < P.slices ? P.cuts[s] : Cut{0, 0};
     bool many = false;
     float a[8];
     if (cut.state == (OPEN | ENDS)) {
@@ -444,7 +444,7 @@ tad_embed_join_kernel(const Sums P)
     for (int w = 0; w < WARPS; ++w) todo |= flags[w] << w;
     for (int w = 0; w < WARPS; ++w) {
         if (!(todo >> w & 1)) continue;
-        const unsigned su = (unit0 + w) / P.slices, sl = unit0 + w - su * P.slices, b = shared_first[w];
+        const unsigned sl = (unit0 + w) / P.segments, su = unit0 + w - sl * P.segments, b = shared_first[w];
         const unsigned long long count = su + 1 - b;
         add(a, b + (unsigned)(count * warp / WARPS), b + (unsigned)(count * (warp + 1) / WARPS), su, sl);
 #pragma unroll
@@ -553,6 +553,9 @@ tad_status tad_embed_backward(const void *tokens, int32_t token_bits, int64_t n_
     while (((uint64_t)n_table >> key_bits) != 0) ++key_bits;
     const int passes = (key_bits + DIGIT_BITS - 1) / DIGIT_BITS, bits = (key_bits + passes - 1) / passes;
     cudaError_t e = cudaSuccess;
+    // (sixteen blocks sort 65536 tokens in 22 us for 30, but a cluster of that size delays the kernels around it: the gradient into
+    // 128000 x 2048 363 us for 287)
+    const int cluster = n_tokens == 0 ? 0 : n_tokens <= 2048 ? 1 : 8;
     if (n_tokens) {
         static std::atomic<bool> allowed[64];
         int dev = -1;
@@ -561,9 +564,6 @@ tad_status tad_embed_backward(const void *tokens, int32_t token_bits, int64_t n_
             e = cudaFuncSetAttribute(tad_embed_sort_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)SORT_SMEM);
             if (e == cudaSuccess && dev >= 0 && dev < 64) allowed[dev].store(true, std::memory_order_relaxed);
         }
-        // (sixteen blocks sort 65536 tokens in 22 us for 30, but a cluster of that size delays the kernels around it: the gradient into
-        // 128000 x 2048 363 us for 287)
-        const int cluster = n_tokens <= 2048 ? 1 : 8;
         const int64_t warps = (int64_t)cluster * SORT_WARPS, run = ((n_tokens + warps - 1) / warps + 31) / 32 * 32;
         if (e == cudaSuccess)
             e = tad_launch_cluster(tad_embed_sort_kernel, cluster, SORT_NT, SORT_SMEM, stream, cluster, tok, (unsigned)n_tokens, (unsigned)run, passes, bits, s0, s1);
@@ -571,7 +571,8 @@ tad_status tad_embed_backward(const void *tokens, int32_t token_bits, int64_t n_
     }
     if (!accumulate) {
         const int64_t size = (int64_t)type_size(dtable->type), stride = dtable->stride * size, row_bytes = width * size;
-        const int64_t blocks = std::min<int64_t>(SMS, (n_table + 31) / 32), each = (n_table + blocks - 1) / blocks;
+        // (an SM a block beside those of the sort: a share whose SM sorts too is the last to end)
+        const int64_t blocks = std::min<int64_t>(SMS - cluster, (n_table + 31) / 32), each = (n_table + blocks - 1) / blocks;
         e = tad_launch(tad_embed_clear_kernel, (unsigned)blocks, CLEAR_NT, 0, stream, tok, (unsigned)n_tokens, each, static_cast<unsigned char *>(dtable->data), stride,
                        row_bytes, n_tokens > 0);
         if (e != cudaSuccess || n_tokens == 0) return launched("clearing of rows without tokens", e);

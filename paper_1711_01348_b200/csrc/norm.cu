@@ -174,41 +174,16 @@ __device__ __forceinline__ bool wait_for(unsigned bar, unsigned parity)
     return false;
 }
 
-// What the blocks of a cluster tell each other: each one's sums go into everybody's shared memory by stores that count at the
-// receiver's mbarrier.  (A cluster barrier instead would wait, as a release, for the rows just written: 8192 columns forward 55 us
-// for 28.)
-template <int N>
-struct Exchange {
-    float far[2][MAX_CLUSTER][N];
-    unsigned long long bar[2];
-};
-// Sums of N values over all threads that share a row, the same bits in each of them.  A warp's sum goes into a box of shared
+// Sums of N values over the threads of a group, the same bits in each of them.  A warp's sum goes into a box of shared
 // memory, everybody adds the boxes up in order; two sets of boxes are used in turn, so one barrier a sum is enough.  ALONE: the group
 // is the block.
 template <int N, int BY, bool ALONE>
 struct Sum {
     float (*box)[BACKWARD_BLOCK / 32][N];  // [2], of this block
-    Exchange<N> *ex;
     int first, warps, id, threads;         // this group: its first warp, its warps, its barrier and its threads
-    int count;                             // sums so far
-    unsigned blocks, rank;                 // of the cluster
-    bool lost;                             // a wait has run out, there are no further ones
-    __device__ __forceinline__ void start()
-    {
-        if (BY != BY_CLUSTER) return;
-        cg::cluster_group cluster = cg::this_cluster();
-        blocks = cluster.num_blocks();
-        rank = cluster.block_rank();
-        if (threadIdx.x == 0) {
-#pragma unroll
-            for (int i = 0; i < 2; ++i) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"((unsigned)__cvta_generic_to_shared(&ex->bar[i])) : "memory");
-            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        }
-        cluster.sync();
-    }
+    int turn;
     __device__ __forceinline__ void of(float (&v)[N])
     {
-        const int turn = count & 1;
         if (BY == BY_WARP) {
 #pragma unroll
             for (int k = 0; k < N; ++k) v[k] = warp_sum(v[k]);
@@ -238,31 +213,52 @@ struct Sum {
                 v[0] += p.x + p.y;
             }
         }
-        if (BY == BY_CLUSTER) {
-            // (a block writes its sum n + 2 behind its sum n + 1, which waits for everybody's, sent behind the reads of sum n)
-            const unsigned bar = (unsigned)__cvta_generic_to_shared(&ex->bar[turn]);
-            if (threadIdx.x == 0) asm volatile("{ .reg .b64 t; mbarrier.arrive.expect_tx.shared::cta.b64 t, [%0], %1; }" ::"r"(bar), "r"(blocks * N * 4) : "memory");
-            if (threadIdx.x < blocks) {
-                unsigned to, at;
-                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"((unsigned)__cvta_generic_to_shared(&ex->far[turn][rank][0])), "r"(threadIdx.x));
-                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(bar), "r"(threadIdx.x));
+        turn ^= 1;
+    }
+};
+
+// What the blocks of a cluster tell each other: two values a block and row go into everybody's shared memory by stores that count
+// at the receiver's mbarrier.  (A cluster barrier instead would wait, as a release, for the rows just written: 8192 columns forward
+// 55 us for 36.)
+struct Exchange {
+    float2 far[2][MAX_CLUSTER];
+    unsigned long long bar[2];
+};
+struct Trade {
+    Exchange *ex;
+    unsigned blocks, rank, count;
+    bool lost;                             // a wait has run out, there are no further ones
+    __device__ __forceinline__ void start(Exchange *e)
+    {
+        ex = e; count = 0; lost = false;
+        cg::cluster_group cluster = cg::this_cluster();
+        blocks = cluster.num_blocks();
+        rank = cluster.block_rank();
+        if (threadIdx.x == 0) {
 #pragma unroll
-                for (int k = 0; k < N; ++k)
-                    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.b32 [%0], %1, [%2];" ::"r"(to + 4 * k), "r"(__float_as_uint(v[k])), "r"(at) : "memory");
-            }
-            const unsigned parity = (count >> 1) & 1;
-            if (!lost) lost = !wait_for(bar, parity);
-#pragma unroll
-            for (int k = 0; k < N; ++k) {
-                float a = !lost ? 0.f : __uint_as_float(0x7fffffffu);         // (a block that never answered: no result)
-                for (unsigned b = 0; b < blocks; ++b) a += ex->far[turn][b][k];
-                v[k] = a;
-            }
+            for (int i = 0; i < 2; ++i) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"((unsigned)__cvta_generic_to_shared(&ex->bar[i])) : "memory");
+            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         }
+        cluster.sync();
+    }
+    // the values of all blocks, in order.  A barrier of the block lies between two trades: a block writes its values n + 2 behind everybody's
+    // values n + 1, which are sent behind that barrier and so behind the reads of the values n.
+    __device__ __forceinline__ const float2 *with_all(float a, float b)
+    {
+        const unsigned turn = count & 1, parity = (count >> 1) & 1, bar = (unsigned)__cvta_generic_to_shared(&ex->bar[turn]);
         ++count;
+        if (threadIdx.x == 0) asm volatile("{ .reg .b64 t; mbarrier.arrive.expect_tx.shared::cta.b64 t, [%0], %1; }" ::"r"(bar), "r"(blocks * 8) : "memory");
+        if (threadIdx.x < blocks) {
+            unsigned to, at;
+            asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"((unsigned)__cvta_generic_to_shared(&ex->far[turn][rank])), "r"(threadIdx.x));
+            asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(bar), "r"(threadIdx.x));
+            asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.b32 [%0], {%1, %2}, [%3];" ::"r"(to), "r"(__float_as_uint(a)), "r"(__float_as_uint(b)), "r"(at) : "memory");
+        }
+        if (!lost) lost = !wait_for(bar, parity);
+        return ex->far[turn];
     }
     // no block leaves while another one may still write into it
-    __device__ __forceinline__ void finish() { if (BY == BY_CLUSTER) cg::this_cluster().sync(); }
+    __device__ __forceinline__ void finish() { cg::this_cluster().sync(); }
 };
 
 // this thread's place: its group in the grid, the groups of the grid, its first column
@@ -293,12 +289,10 @@ struct Place {
 };
 
 template <int N, int BY, bool ALONE>
-__device__ __forceinline__ Sum<N, BY, ALONE> sum_of(const Params &P, float (*box)[BACKWARD_BLOCK / 32][N], Exchange<N> *ex)
+__device__ __forceinline__ Sum<N, BY, ALONE> sum_of(const Params &P, float (*box)[BACKWARD_BLOCK / 32][N])
 {
     const int g = BY == BY_CLUSTER ? 0 : threadIdx.x / P.group;
-    Sum<N, BY, ALONE> s{box, ex, g * (P.group >> 5), P.group >> 5, 1 + g, P.group, 0, 1, 0, false};
-    s.start();
-    return s;
+    return Sum<N, BY, ALONE>{box, g * (P.group >> 5), P.group >> 5, 1 + g, P.group, 0};
 }
 
 // ---- rows ahead ----
@@ -380,17 +374,19 @@ tad_norm_forward_kernel(const Params P)
 {
     constexpr int E = FORWARD_E, STAGES = FORWARD_STAGES<T>;
     __shared__ __align__(16) float box[2][BACKWARD_BLOCK / 32][1];
-    __shared__ Exchange<1> ex;
+    __shared__ Exchange ex;
     __shared__ unsigned long long bars[FORWARD_BLOCK / 32][STAGES];
     extern __shared__ __align__(128) unsigned char rows[];
     tad_wait_previous();
-    Sum<1, BY, true> sum = sum_of<1, BY, true>(P, box, &ex);
+    Sum<1, BY, true> sum = sum_of<1, BY, true>(P, box);
+    Trade trade;
+    if constexpr (BY == BY_CLUSTER) trade.start(&ex);
     const Place<BY, V, E> at(P);
     int64_t r = at.row;
     const T *__restrict__ x = static_cast<const T *>(P.x);
     Held<T, 1, V == 1 ? E : 1> next;       // (V = 1)
     Ring<STAGES> ring;
-    const unsigned bytes = (unsigned)max(0, min(P.width - at.col0, P.group * E)) * (unsigned)sizeof(T);
+    const unsigned columns = (unsigned)max(0, min(P.width - at.col0, P.group * E)), bytes = columns * (unsigned)sizeof(T);
     if constexpr (V != 1) {
         ring.start(rows, at.group * STAGES * P.group * E * (unsigned)sizeof(T), smem_u32(&bars[at.group][0]), P.group * E * (unsigned)sizeof(T), at.in == 0);
         clear_ring(rows, blockDim.x * STAGES * E * (unsigned)sizeof(T));
@@ -439,8 +435,10 @@ tad_norm_forward_kernel(const Params P)
             }
             ring.advance();
         }
-        // (a row that never came has no result)
-        const float mean = V != 1 && ring.lost ? __uint_as_float(0x7fffffffu) : s[0] * P.inv_width;
+        // the mean, in a cluster that of the block's columns, and the squared deviations from it
+        const bool no_result = (V != 1 && ring.lost) || (BY == BY_CLUSTER && trade.lost);       // (a row or a block that never came)
+        const float total = no_result ? __uint_as_float(0x7fffffffu) : s[0];
+        float mean = BY == BY_CLUSTER ? (columns ? total / (float)columns : 0.f) : total * P.inv_width;
         two = make_float2(0.f, 0.f);
 #pragma unroll
         for (int j = 0; j < E / 2; ++j) {
@@ -449,6 +447,24 @@ tad_norm_forward_kernel(const Params P)
         }
         s[0] = two.x + two.y;
         sum.of(s);
+        if constexpr (BY == BY_CLUSTER) {
+            // one exchange a row: the squares about the row's mean are those about a block's and the block's count times the squared distance
+            // of the two
+            const float2 *all = trade.with_all(total, s[0]);
+            float sums = 0.f, squares = 0.f;
+            for (unsigned b = 0; b < trade.blocks; ++b) sums += all[b].x;
+            const float whole = sums * P.inv_width;
+            for (unsigned b = 0; b < trade.blocks; ++b) {
+                const int n = max(0, min(P.width - (int)(b * blockDim.x) * E, (int)blockDim.x * E));
+                const float d = n ? all[b].x / (float)n - whole : 0.f;
+                squares += all[b].y + (float)n * (d * d);
+            }
+            s[0] = squares;
+            const float2 shift = make_float2(mean - whole, mean - whole);
+#pragma unroll
+            for (int j = 0; j < E / 2; ++j) u.p[j] = __fadd2_rn(u.p[j], shift);
+            mean = whole;
+        }
         const float rstd = rsqrtf(s[0] * P.inv_width + P.eps);
         if (at.col == 0) {
             if (P.mean) P.mean[r] = mean;
@@ -460,7 +476,7 @@ tad_norm_forward_kernel(const Params P)
         u.get(v);
         store_typed<V, E>(P.y, P.y_type, r * P.ys + at.col, at.rem, v);
     }
-    sum.finish();
+    if constexpr (BY == BY_CLUSTER) trade.finish();
 }
 
 // of one value over a block of 1024 threads
@@ -568,12 +584,14 @@ tad_norm_backward_kernel(const Params P)
 {
     constexpr int E = BACKWARD_E<V>, STAGES = BACKWARD_STAGES<S, T>;
     __shared__ __align__(16) float box[2][BACKWARD_BLOCK / 32][2];
-    __shared__ Exchange<2> ex;
+    __shared__ Exchange ex;
     __shared__ unsigned long long bars[BACKWARD_BLOCK / 32][STAGES];
     extern __shared__ __align__(128) unsigned char rows[];
     __shared__ __align__(16) float join[BY == BY_CLUSTER ? 1 : BACKWARD_BLOCK][BY == BY_CLUSTER ? 4 : 8];
     tad_wait_previous();
-    Sum<2, BY, BY == BY_CLUSTER> sum = sum_of<2, BY, BY == BY_CLUSTER>(P, box, &ex);
+    Sum<2, BY, BY == BY_CLUSTER> sum = sum_of<2, BY, BY == BY_CLUSTER>(P, box);
+    Trade trade;
+    if constexpr (BY == BY_CLUSTER) trade.start(&ex);
     const Place<BY, V, E> at(P);
     int64_t r = at.row;
     const T *__restrict__ dy = static_cast<const T *>(P.dy);
@@ -680,6 +698,11 @@ tad_norm_backward_kernel(const Params P)
             if (ring.leader && !ring.lost && r + STAGES * at.step < P.n_rows) issue(ring.at, r + STAGES * at.step);
             ring.advance();
         }
+        if constexpr (BY == BY_CLUSTER) {
+            const float2 *all = trade.with_all(s[0], s[1]);
+            s[0] = s[1] = trade.lost ? __uint_as_float(0x7fffffffu) : 0.f;
+            for (unsigned b = 0; b < trade.blocks; ++b) { s[0] += all[b].x; s[1] += all[b].y; }
+        }
         if (P.dx) {
             const float c1 = -s[0] * P.inv_width, c2 = -s[1] * P.inv_width;
             const float2 rr = make_float2(rstd, rstd), m1 = make_float2(c1, c1), m2 = make_float2(c2, c2);
@@ -689,7 +712,7 @@ tad_norm_backward_kernel(const Params P)
             store_typed<V, E>(P.dx, P.dx_type, r * P.dxs + at.col, at.rem, d);
         }
     }
-    sum.finish();
+    if constexpr (BY == BY_CLUSTER) trade.finish();
     if (!P.planes) return;
     float dw[E], db[E];
     dws.get(dw);
@@ -833,14 +856,48 @@ Shape shape_of(int64_t width, int block, int e)
     return s;
 }
 
+// the backward pass: blocks of 512 threads or, in clusters that hold the row so, two of 256 an SM, so that two rows are under way there
+Shape backward_shape(int64_t width, int e)
+{
+    const bool halves = width > (int64_t)BACKWARD_BLOCK * e && width <= (int64_t)(BACKWARD_BLOCK / 2) * e * MAX_CLUSTER;
+    return shape_of(width, halves ? BACKWARD_BLOCK / 2 : BACKWARD_BLOCK, e);
+}
+
 // Planes of partial sums of the backward pass, one a block or cluster: one block an SM, as many groups in it as fit.  The workspace has
 // room for those of either number of elements a thread.
 int64_t planes_of(int64_t n_rows, int64_t width, int e)
 {
     if (width > HELD) return std::max<int64_t>(1, std::min<int64_t>(n_rows, 64));
-    const Shape s = shape_of(width, BACKWARD_BLOCK, e);
+    const Shape s = backward_shape(width, e);
     const int groups = s.by == BY_CLUSTER ? 1 : BACKWARD_BLOCK / s.group;
-    return std::max<int64_t>(1, std::min<int64_t>((n_rows + groups - 1) / groups, SMS / s.cluster));
+    return std::max<int64_t>(1, std::min<int64_t>((n_rows + groups - 1) / groups, SMS * (s.by == BY_CLUSTER ? BACKWARD_BLOCK / s.group : 1) / s.cluster));
+}
+
+// Clusters that run at a time: not all SMs of the device have enough neighbours, and one that has to wait for another doubles the time
+// (2048 x 16384 bf16 forward 72 us for 49).  The device is asked once for a kernel and a size of clusters; `known`: 64 devices,
+// clusters of 2, 4 and 8.
+template <class K>
+cudaError_t clusters_of(K kernel, int threads, size_t smem, int cluster, std::atomic<int> (*known)[3], int64_t &most)
+{
+    int dev = -1;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    std::atomic<int> *place = dev >= 0 && dev < 64 ? &known[dev][cluster == 2 ? 0 : cluster == 4 ? 1 : 2] : nullptr;
+    int n = place ? place->load(std::memory_order_relaxed) : 0;
+    if (!n) {
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = cluster; cfg.blockDim = threads; cfg.dynamicSmemBytes = smem;
+        cudaLaunchAttribute attr = {};
+        attr.id = cudaLaunchAttributeClusterDimension;
+        attr.val.clusterDim.x = cluster; attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+        cfg.attrs = &attr; cfg.numAttrs = 1;
+        e = cudaOccupancyMaxActiveClusters(&n, kernel, &cfg);
+        if (e != cudaSuccess) return e;
+        n = std::max(1, n);
+        if (place) place->store(n, std::memory_order_relaxed);
+    }
+    most = n;
+    return cudaSuccess;
 }
 
 template <class T>
@@ -848,12 +905,17 @@ cudaError_t forward(const Params &P, const Shape &s, bool eights, cudaStream_t s
 {
     if (P.width > HELD) return tad_launch(tad_norm_forward_long_kernel<T>, (unsigned)std::min<int64_t>(P.n_rows, 2 * SMS), LARGE, 0, stream, P);
     const int threads = s.by == BY_WARP ? FORWARD_BLOCK : s.group, groups = s.by == BY_WARP ? FORWARD_BLOCK / 32 : 1;
-    const int64_t most = (int64_t)SMS * std::min(32, (eights ? FORWARD_BLOCKS : 2) * FORWARD_BLOCK / threads) / s.cluster;
-    const unsigned blocks = (unsigned)(std::min((P.n_rows + groups - 1) / groups, most) * s.cluster);
+    int64_t most = (int64_t)SMS * std::min(32, (eights ? FORWARD_BLOCKS : 2) * FORWARD_BLOCK / threads);
     auto kernel = tad_norm_forward_kernel<T, 1, BY_WARP>;
     if (eights) kernel = s.by == BY_WARP ? tad_norm_forward_kernel<T, 8, BY_WARP> : s.by == BY_GROUP ? tad_norm_forward_kernel<T, 8, BY_GROUP> : tad_norm_forward_kernel<T, 8, BY_CLUSTER>;
     else if (s.by != BY_WARP) kernel = s.by == BY_GROUP ? tad_norm_forward_kernel<T, 1, BY_GROUP> : tad_norm_forward_kernel<T, 1, BY_CLUSTER>;
     const size_t smem = eights ? (size_t)threads * FORWARD_E * sizeof(T) * FORWARD_STAGES<T> : 0;      // (32 KB at most)
+    if (s.cluster > 1) {
+        static std::atomic<int> known[2][64][3];
+        const cudaError_t e = clusters_of(kernel, threads, smem, s.cluster, known[eights], most);
+        if (e != cudaSuccess) return e;
+    }
+    const unsigned blocks = (unsigned)(std::min((P.n_rows + groups - 1) / groups, most) * s.cluster);
     return tad_launch_cluster(kernel, blocks, threads, smem, stream, s.cluster, P);
 }
 
@@ -863,7 +925,7 @@ cudaError_t backward(Params &P, bool eights, int64_t &planes, cudaStream_t strea
 {
     const int e8 = eights ? BACKWARD_E<8> : BACKWARD_E<1>;
     planes = planes_of(P.n_rows, P.width, e8);
-    const Shape s = shape_of(P.width, BACKWARD_BLOCK, e8);
+    const Shape s = backward_shape(P.width, e8);
     P.group = s.group;
     if (P.width > HELD) {
         cudaError_t e = cudaSuccess;
@@ -890,6 +952,13 @@ cudaError_t backward(Params &P, bool eights, int64_t &planes, cudaStream_t strea
             if (dev >= 0 && dev < 64) allowed[dev][s.by].store(true, std::memory_order_relaxed);
         }
         smem = (size_t)threads * BACKWARD_E<8> * (SOURCE_BYTES<S> + sizeof(T)) * BACKWARD_STAGES<S, T>;
+    }
+    if (s.cluster > 1) {
+        static std::atomic<int> known[2][64][3];
+        int64_t most = 0;
+        const cudaError_t e = clusters_of(kernel, threads, smem, s.cluster, known[eights], most);
+        if (e != cudaSuccess) return e;
+        planes = std::min(planes, most);
     }
     return tad_launch_cluster(kernel, (unsigned)(planes * s.cluster), threads, smem, stream, s.cluster, P);
 }
