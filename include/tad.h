@@ -324,7 +324,7 @@ typedef struct {
  * of either, which pack8 may have rounded up to 2^128, come back as infinities).
  * tad_repack8 packs the transpose of a packed matrix: in is n_rows x width, out width x n_rows with blocks of 128 along
  * what were the rows of `in` - the form in which a product that sums over the rows (the gradient of a weight) reads it.
- * NaNs stay; the values of `in` are taken as they are (q 2^k in fp32) and rounded once more.
+ * NaNs stay; the values of `in` are taken as they are (q 2^k in fp32) and rounded once more.  n_rows < 2^24 there (a width of out).
  */
 tad_status tad_pack8(const tad_rows *x, int64_t n_rows, int64_t width, const tad_packed *out, void *cuda_stream);
 tad_status tad_unpack8(const tad_packed *in, int64_t n_rows, int64_t width, const tad_rows *x, void *cuda_stream);

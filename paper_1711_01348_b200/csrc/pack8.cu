@@ -287,14 +287,16 @@ tad_repack8_kernel(const uint8_t *__restrict__ q, int64_t qs, const uint8_t *__r
 }
 
 struct Launch { unsigned blocks, chunks; int cb; };
-Launch cover(int64_t n_rows, int64_t n_blocks, int own)
+// false: more blocks than a launch has (of matrices beyond any memory)
+bool cover(int64_t n_rows, int64_t n_blocks, int own, Launch &l)
 {
-    Launch l{0, 0, 0};
+    l = Launch{0, 0, 0};
     while ((NT >> own >> l.cb) > 1 && (int64_t(1) << l.cb) < n_blocks) ++l.cb;
     l.chunks = (unsigned)((n_blocks + (1 << l.cb) - 1) >> l.cb);
     const int64_t rows = ROWS * (NT >> own >> l.cb);
-    l.blocks = (unsigned)((n_rows + rows - 1) / rows * l.chunks);
-    return l;
+    const int64_t blocks = (n_rows + rows - 1) / rows * l.chunks;
+    l.blocks = (unsigned)blocks;
+    return blocks < MAX_ROWS;
 }
 
 // a warp a row and ODD blocks of 128
@@ -313,7 +315,8 @@ tad_status tad_launch_pack8(const tad_rows *x, int64_t n_rows, int64_t width, co
 {
     cudaError_t e = cudaSuccess;
     if (by_eights(x)) {
-        const Launch l = cover(n_rows, tadr::blocks_of(width), OWN_PACK);
+        Launch l;
+        if (!cover(n_rows, tadr::blocks_of(width), OWN_PACK, l)) { tad::set_error("pack8: too many blocks"); return TAD_ERR_UNSUPPORTED; }
         TAD_WITH_TYPE(x->type, T,
             e = tad_launch(tad_pack8_kernel<T>, l.blocks, NT, 0, stream, static_cast<const T *>(x->data), x->stride, n_rows, (int)width, l.cb, l.chunks, out->q,
                            out->q_stride, out->scale, out->scale_stride));
@@ -345,7 +348,8 @@ tad_status tad_unpack8(const tad_packed *in, int64_t n_rows, int64_t width, cons
     const cudaStream_t stream = (cudaStream_t)cuda_stream;
     cudaError_t e = cudaSuccess;
     if (by_eights(x)) {
-        const Launch l = cover(n_rows, blocks_of(width), OWN_UNPACK);
+        Launch l;
+        if (!cover(n_rows, blocks_of(width), OWN_UNPACK, l)) { tad::set_error("unpack8: too many blocks"); return TAD_ERR_UNSUPPORTED; }
         TAD_WITH_TYPE(x->type, T,
             e = tad_launch(tad_unpack8_kernel<T>, l.blocks, NT, 0, stream, in->q, in->q_stride, in->scale, in->scale_stride, n_rows, (int)width, l.cb, l.chunks,
                            static_cast<T *>(x->data), x->stride));

@@ -1,5 +1,5 @@
 """Layer norm against its formula in 64 bits: every type, odd widths, strides and offsets, both sides of each change of kernel
-(512 columns a warp, 4096 with weights in registers, 16384 in a block), few and many rows, from x and from its 8-bit form.
+(512 columns a warp, 4096 or 8192 a block, 32768 a cluster), few and many rows, from x and from its 8-bit form.
 
 Tolerances: u = 2^-24 is the rounding of an operation, a sum over a row passes at most depth(width) of them (16 elements or
 width / 1024 a thread, ten levels of shuffles), a result is rounded to its type once."""
@@ -13,7 +13,9 @@ from paper_1711_01348_b200 import layernorm_backward, layernorm_forward, layerno
 from tests.operator_util import (U, Matrix, PackedMatrix, assert_within, half_step, pack_reference, same_codes, stream,  # noqa: E402
                                  tiny, unpack_reference, workspace)
 
-WIDTHS = [1, 2, 7, 8, 33, 128, 500, 512, 513, 520, 1001, 1024, 2823, 4096, 4097, 4104, 8192, 11001, 16384, 16385, 20000]
+# (either side of a warp, a block, clusters of 2, 4 and 8 blocks of either pass, and of the longest row that a cluster holds)
+WIDTHS = [1, 2, 7, 8, 33, 128, 500, 512, 513, 520, 1001, 1024, 2823, 4096, 4097, 4104, 8192, 8200, 11001, 16384, 16385, 16392, 20000, 32767, 32768,
+          32769, 32776, 40000]
 
 
 def depth(width):
@@ -121,7 +123,7 @@ def test_types_strides_offsets(kind, ykind, wkind, width, pad, offset):
     _run(13, width, kind, ykind, wkind, pad, offset)
 
 
-@pytest.mark.parametrize("width", [8, 120, 128, 136, 512, 777, 1024, 4096, 5000, 8192, 16384, 17000])
+@pytest.mark.parametrize("width", [8, 120, 128, 136, 512, 777, 1024, 4096, 5000, 8192, 8201, 16384, 17000, 17001, 33000, 33001])
 @pytest.mark.parametrize("kind", ["f32", "bf16"])
 def test_from_the_checkpoint(width, kind):
     _run(19, width, kind, packed=True, pad=0 if width % 16 else 8)

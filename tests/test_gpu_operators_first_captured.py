@@ -1,0 +1,56 @@
+"""The first calls of a process may be captured: what a kernel needs once on a device (attributes, sizes of clusters, the driver's entry
+points) is no work of a stream.  In a process of its own, where nothing has been called before."""
+import subprocess
+import sys
+
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+SCRIPT = """
+import os, sys
+sys.path.insert(0, os.getcwd())
+import torch
+import paper_1711_01348_b200 as tad
+def rows(t): return tad.Rows(t.data_ptr(), t.stride(0), "f32")
+def eight(n, w):
+    q, s = torch.zeros((n, -(-w // 16) * 16), dtype=torch.uint8, device="cuda"), torch.full((n, -(-(-(-w // 128)) // 4) * 4), 127, dtype=torch.uint8, device="cuda")
+    return q, s, tad.Packed(q.data_ptr(), s.data_ptr(), q.stride(0), s.stride(0))
+n, d, v = 3000, 9000, 50
+x, dy = torch.randn((n, d), device="cuda"), torch.randn((n, d), device="cuda")
+y, dx, dt = torch.empty_like(x), torch.empty_like(x), torch.empty((v, d), device="cuda")
+p, o = torch.empty((n, n), device="cuda"), torch.empty((1, n), device="cuda")
+mean, rstd, dw, db = torch.empty(n, device="cuda"), torch.empty(n, device="cuda"), torch.empty((1, d), device="cuda"), torch.empty((1, d), device="cuda")
+tok = torch.randint(0, v, (n,), device="cuda", dtype=torch.int32)
+a, b = eight(n, d), eight(d, n)
+need = max(tad.layernorm_workspace_bytes(n, d), tad.embed_workspace_bytes(n, v, d), tad.matmul8_workspace_bytes(n, n, d), 256)
+ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+room = dict(workspace_ptr=ws.data_ptr(), workspace_bytes=need)
+def step(st):
+    tad.layernorm_forward(rows(x), n, d, rows(y), mean_ptr=mean.data_ptr(), rstd_ptr=rstd.data_ptr(), checkpoint=a[2], stream=st)
+    tad.layernorm_backward(rows(dy), rows(x), None, n, d, mean.data_ptr(), rstd.data_ptr(), rows(dx), dweight=rows(dw), dbias=rows(db), stream=st, **room)
+    tad.matmul8(a[2], a[2], n, n, d, rows(p), stream=st, **room)
+    tad.matmul8(a[2], a[2], 1, n, d, rows(o), stream=st, **room)
+    tad.repack8(a[2], n, d, b[2], stream=st)
+    tad.embed_backward(tok.data_ptr(), 32, n, rows(dy), v, d, 1.0, rows(dt), stream=st, **room)
+    tad.embed_forward(tok.data_ptr(), 32, n, rows(dt), v, d, 1.0, rows(x), stream=st)
+keep = x.clone()
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g):
+    step(torch.cuda.current_stream().cuda_stream)
+g.replay()
+torch.cuda.synchronize()
+out = [y, dx, dt, p, o, mean, rstd, dw, db, x, a[0], a[1], b[0], b[1]]
+got = [t.clone() for t in out]
+x.copy_(keep)
+for t in out[:9]: t.fill_(float("nan"))
+step(torch.cuda.current_stream().cuda_stream)
+torch.cuda.synchronize()
+assert all(torch.equal(s, t) for s, t in zip(got, out)) and all(bool(torch.isfinite(t.float()).all()) for t in out[:9])
+print("same")
+"""
+
+
+def test_first_calls_captured():
+    r = subprocess.run([sys.executable, "-c", SCRIPT], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and r.stdout.strip().endswith("same"), r.stdout + r.stderr

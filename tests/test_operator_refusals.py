@@ -97,6 +97,10 @@ def test_arguments_of_their_own():
     _refused(lambda: layernorm_backward(r, None, None, 3, 100, P, P, r))       # none
     _refused(lambda: layernorm_backward(r, r, None, 3, 100, 0, P, r))
     _refused(lambda: layernorm_backward(r, r, None, 3, 100, P, 0, r))
+    _refused(lambda: layernorm_backward(r, r, None, 3, 100, P + 2, P, r))
+    _refused(lambda: layernorm_backward(r, r, None, 3, 100, P, P + 1, r))
+    _refused(lambda: layernorm_forward(r, 3, 100, r, mean_ptr=P + 2))
+    _refused(lambda: layernorm_forward(r, 3, 100, r, rstd_ptr=P + 2))
     _refused(lambda: embed_forward(P, 16, 3, r, 7, 100, 1.0, r))
     _refused(lambda: embed_forward(0, 32, 3, r, 7, 100, 1.0, r))
     _refused(lambda: embed_forward(P + 4, 64, 3, r, 7, 100, 1.0, r))
@@ -109,6 +113,13 @@ def test_arguments_of_their_own():
     _refused(lambda: pack8(big, 1 << 31, 100, _p()), "TAD_ERR_UNSUPPORTED")
     _refused(lambda: layernorm_forward(big, 3, 1 << 24, big), "TAD_ERR_UNSUPPORTED")
     _refused(lambda: embed_forward(P, 32, 3, big, 1 << 31, 100, 1.0, big), "TAD_ERR_UNSUPPORTED")
+    far = Packed(P, P, 1 << 30, 1 << 20)
+    _refused(lambda: repack8(far, 1 << 24, 100, far), "TAD_ERR_UNSUPPORTED")
+    # more blocks than a launch has: sizes beyond any memory, and the accesses with them
+    _refused(lambda: pack8(big, (1 << 31) - 1, (1 << 24) - 1, far), "TAD_ERR_UNSUPPORTED")
+    _refused(lambda: unpack8(far, (1 << 31) - 1, (1 << 24) - 1, big), "TAD_ERR_UNSUPPORTED")
+    _refused(lambda: pack8(Rows(P + 4, 1 << 40, "f32"), (1 << 31) - 1, (1 << 24) - 1, far), "TAD_ERR_UNSUPPORTED")
+    _refused(lambda: matmul8(far, far, (1 << 31) - 1, 1 << 20, 100, big, **ROOM), "TAD_ERR_UNSUPPORTED")
 
 
 @fake
