@@ -251,7 +251,7 @@ struct Sums {
     int64_t dys;
     void *dtable;
     int64_t ds;
-    int type, accumulate;
+    int accumulate;
     unsigned n, n_table, segments, slices, each;           // each: positions of a segment
     int width;
     float factor;
@@ -259,72 +259,80 @@ struct Sums {
     Cut *cuts;
 };
 
-// V = 8: a lane's columns are neighbours; V = 1: 32 apart
-template <int V> __device__ __forceinline__ int column_of(int lane, int i) { return V == 8 ? lane * 8 : lane + 32 * i; }
+// Eight columns a lane: V = 8, neighbours; V = 1, 32 apart.  A piece of a row of dy, or the sums (two columns an instruction).
+template <int V> __device__ __forceinline__ constexpr int place(int i) { return V == 8 ? 0 : 32 * i; }
+template <int V> __device__ __forceinline__ int first_column(int lane) { return V == 8 ? lane * 8 : lane; }
 
 template <class T, int V>
 struct RowPiece {
     Piece<T, V> p[8 / V];
-    __device__ __forceinline__ void load(const T *__restrict__ row, int lane, int columns)
+    // from the lane's first column on; whole: all of the slice's columns exist
+    __device__ __forceinline__ void load(const T *__restrict__ at, int rem, bool whole)
     {
 #pragma unroll
         for (int i = 0; i < 8 / V; ++i) {
-            p[i].zero();
-            if (column_of<V>(lane, i) < columns) p[i].load(row + column_of<V>(lane, i));
+            if (whole) p[i].load(at + place<V>(i));
+            else {
+                p[i].zero();
+                if (place<V>(i) < rem) p[i].load(at + place<V>(i));
+            }
         }
     }
-    __device__ __forceinline__ void add_to(float (&a)[8]) const
+    __device__ __forceinline__ void add_to(float2 (&a)[4]) const
     {
+        float v[8];
 #pragma unroll
         for (int i = 0; i < 8 / V; ++i) {
-            float v[V];
-            p[i].get(v);
+            float f[V];
+            p[i].get(f);
 #pragma unroll
-            for (int j = 0; j < V; ++j) a[i * V + j] += v[j];
+            for (int j = 0; j < V; ++j) v[i * V + j] = f[j];
         }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) a[j] = __fadd2_rn(a[j], make_float2(v[2 * j], v[2 * j + 1]));
     }
 };
-
-// the finished sum of a row
-template <int V>
-__device__ __forceinline__ void write_row(const Sums &P, unsigned row, int c0, int lane, int columns, const float (&a)[8])
+__device__ __forceinline__ void clear(float2 (&a)[4])
 {
-    const int64_t at = (int64_t)row * P.ds + c0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) a[j] = make_float2(0.f, 0.f);
+}
+
+// the finished sum of a row; to: the lane's first column of the slice in row 0
+template <class O, int V>
+__device__ __forceinline__ void write_row(const Sums &P, O *__restrict__ to, unsigned row, int rem, const float2 (&a)[4])
+{
+    O *at = to + (int64_t)row * P.ds;
 #pragma unroll
     for (int i = 0; i < 8 / V; ++i) {
-        const int c = column_of<V>(lane, i);
-        if (c >= columns) continue;
+        if (place<V>(i) >= rem) continue;
         float v[V];
 #pragma unroll
-        for (int j = 0; j < V; ++j) v[j] = a[i * V + j] * P.factor;
-        auto store = [&](auto *out) {
-            using O = typename std::remove_pointer<decltype(out)>::type;
-            Piece<O, V> o;
-            if (P.accumulate) {
-                float old[V];
-                o.load(out + at + c);
-                o.get(old);
+        for (int j = 0; j < V; ++j) v[j] = ((i * V + j) & 1 ? a[(i * V + j) / 2].y : a[(i * V + j) / 2].x) * P.factor;
+        Piece<O, V> o;
+        if (P.accumulate) {
+            float old[V];
+            o.load(at + place<V>(i));
+            o.get(old);
 #pragma unroll
-                for (int j = 0; j < V; ++j) v[j] += old[j];
-            }
-            o.set(v);
-            o.store(out + at + c);
-        };
-        if (P.type == TAD_F32) store(static_cast<float *>(P.dtable));
-        else if (P.type == TAD_BF16) store(static_cast<__nv_bfloat16 *>(P.dtable));
-        else store(static_cast<__half *>(P.dtable));
+            for (int j = 0; j < V; ++j) v[j] += old[j];
+        }
+        o.set(v);
+        o.store(at + place<V>(i));
     }
 }
 
-// partial sums: eight floats a lane, `place` = segment and slice
-__device__ __forceinline__ void put_part(float *to, size_t place, int lane, const float (&a)[8])
+// partial sums: eight floats a lane, `part` = segment and slice
+__device__ __forceinline__ float *part_at(float *parts, size_t part, int lane) { return parts + part * SLICE + lane * 8; }
+__device__ __forceinline__ void put_part(float *to, const float2 (&a)[4])
 {
     Piece<float, 8> o;
-    o.set(a);
-    o.store(to + place * SLICE + lane * 8);
+    o.a = make_float4(a[0].x, a[0].y, a[1].x, a[1].y);
+    o.b = make_float4(a[2].x, a[2].y, a[3].x, a[3].y);
+    o.store(to);
 }
 
-template <class T, int V>
+template <class T, class O, int V>
 __global__ void __launch_bounds__(NT, SUM_BLOCKS)
 tad_embed_sums_kernel(const Sums P)
 {
@@ -333,25 +341,25 @@ tad_embed_sums_kernel(const Sums P)
     const int lane = threadIdx.x & 31;
     const unsigned unit = blockIdx.x * (NT / 32) + (threadIdx.x >> 5), s = unit / P.slices, slice = unit - s * P.slices;
     if (s >= P.segments) return;
-    const int c0 = (int)slice * SLICE, columns = min(SLICE, P.width - c0);
+    const int column = (int)slice * SLICE + first_column<V>(lane), rem = P.width - column;
+    const bool whole = (int)slice * SLICE + SLICE <= P.width;
     const unsigned beg = (unsigned)min((unsigned long long)P.n, (unsigned long long)s * P.each), end = (unsigned)min((unsigned long long)P.n, (unsigned long long)beg + P.each);
     unsigned row = beg < end ? P.sorted[beg].x : P.n_table;
     const unsigned first = row;
     bool open = beg > 0 && row < P.n_table && P.sorted[beg - 1].x == row, ends = false;
     const bool opened = open;
-    const T *__restrict__ dy = static_cast<const T *>(P.dy) + c0;
-    float a[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) a[e] = 0.f;
+    const T *__restrict__ dy = static_cast<const T *>(P.dy) + column;
+    O *__restrict__ out = static_cast<O *>(P.dtable) + column;
+    float2 a[4];
+    clear(a);
     // the sum of `row` is complete
     auto close = [&] {
         if (open) {
-            put_part(P.head, (size_t)s * P.slices + slice, lane, a);
+            put_part(part_at(P.head, (size_t)s * P.slices + slice, lane), a);
             ends = true;
             open = false;
-        } else write_row<V>(P, row, c0, lane, columns, a);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) a[e] = 0.f;
+        } else write_row<O, V>(P, out, row, rem, a);
+        clear(a);
     };
     // (tokens outside the table are sorted to the end)
     auto positions = [&](unsigned i) { return i < end ? P.sorted[i] : make_uint2(P.n_table, 0); };
@@ -362,28 +370,28 @@ tad_embed_sums_kernel(const Sums P)
         const int count = (int)min(32u, end - i);
 #pragma unroll 1
         for (int u = 0; u < count; u += A) {
-            // some positions, their rows under way before the first is added
+            // some positions, their rows under way before the first is added (behind the segment's end: row 0 once more, not added)
             RowPiece<T, V> p[A];
             unsigned k[A];
 #pragma unroll
             for (int q = 0; q < A; ++q) {
                 k[q] = __shfl_sync(0xffffffffu, here.x, u + q);
-                const unsigned t = __shfl_sync(0xffffffffu, here.y, u + q);
-                p[q].load(dy + (int64_t)t * P.dys, lane, k[q] < P.n_table ? columns : 0);
+                p[q].load(dy + (int64_t)__shfl_sync(0xffffffffu, here.y, u + q) * P.dys, rem, whole);
             }
 #pragma unroll
             for (int q = 0; q < A; ++q) {
+                if (u + q >= count) continue;
                 if (k[q] != row) {
-                    if (row < P.n_table && u + q < count) close();
-                    if (u + q < count) row = k[q];
+                    if (row < P.n_table) close();
+                    row = k[q];
                 }
-                p[q].add_to(a);
+                if (row < P.n_table) p[q].add_to(a);
             }
         }
     }
     // the row that is open at the end
     if (row < P.n_table) {
-        if (end < P.n && P.sorted[end].x == row) put_part(P.tail, (size_t)s * P.slices + slice, lane, a);
+        if (end < P.n && P.sorted[end].x == row) put_part(part_at(P.tail, (size_t)s * P.slices + slice, lane), a);
         else close();
     }
     if (slice == 0 && lane == 0) P.cuts[s] = Cut{first, (opened ? OPEN : 0u) | (ends ? ENDS : 0u)};
@@ -393,7 +401,7 @@ tad_embed_sums_kernel(const Sums P)
 // and slice; where there are many tails, the warps of the block share them (the slices of a segment lie in different blocks then).
 constexpr unsigned MANY = 16;
 
-template <int V>
+template <class O, int V>
 __global__ void __launch_bounds__(NT)
 tad_embed_join_kernel(const Sums P)
 {
@@ -402,23 +410,23 @@ tad_embed_join_kernel(const Sums P)
     __shared__ unsigned shared_first[WARPS];                   // where the block shares the work: the segment that the row begins in
     tad_wait_previous();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    auto add = [&](float (&a)[8], unsigned lo, unsigned hi, unsigned s, unsigned slice) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) a[e] = 0.f;
+    auto add = [&](float2 (&a)[4], unsigned lo, unsigned hi, unsigned s, unsigned slice) {
+        clear(a);
 #pragma unroll 4
         for (unsigned q = lo; q < hi; ++q) {
-            Piece<float, 8> p;
-            float v[8];
-            p.load((q < s ? P.tail : P.head) + ((size_t)q * P.slices + slice) * SLICE + lane * 8);
-            p.get(v);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) a[e] += v[e];
+            RowPiece<float, 8> p;
+            p.load(part_at(q < s ? P.tail : P.head, (size_t)q * P.slices + slice, lane), 8, true);
+            p.add_to(a);
         }
+    };
+    auto write = [&](const float2 (&a)[4], unsigned row, unsigned slice) {
+        const int column = (int)slice * SLICE + first_column<V>(lane);
+        write_row<O, V>(P, static_cast<O *>(P.dtable) + column, row, P.width - column, a);
     };
     const unsigned unit0 = blockIdx.x * WARPS, unit = unit0 + warp, slice = unit / P.segments, s = unit - slice * P.segments;
     const Cut cut = slice < P.slices ? P.cuts[s] : Cut{0, 0};
     bool many = false;
-    float a[8];
+    float2 a[4];
     if (cut.state == (OPEN | ENDS)) {
         // the segment that the row begins in: the last one before s that does not begin inside it
         unsigned b = s;
@@ -432,7 +440,7 @@ tad_embed_join_kernel(const Sums P)
         if (many) { if (lane == 0) shared_first[warp] = b; }
         else {
             add(a, b, s + 1, s, slice);
-            write_row<V>(P, cut.first_row, (int)slice * SLICE, lane, min(SLICE, P.width - (int)slice * SLICE), a);
+            write(a, cut.first_row, slice);
         }
     }
     unsigned todo = 0;
@@ -448,14 +456,14 @@ tad_embed_join_kernel(const Sums P)
         const unsigned long long count = su + 1 - b;
         add(a, b + (unsigned)(count * warp / WARPS), b + (unsigned)(count * (warp + 1) / WARPS), su, sl);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) part[warp][lane * 8 + e] = a[e];
+        for (int e = 0; e < 4; ++e) *reinterpret_cast<float2 *>(&part[warp][lane * 8 + 2 * e]) = a[e];
         __syncthreads();
         if (warp == 0) {
 #pragma unroll
             for (int q = 1; q < WARPS; ++q)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) a[e] += part[q][lane * 8 + e];
-            write_row<V>(P, P.cuts[su].first_row, (int)sl * SLICE, lane, min(SLICE, P.width - (int)sl * SLICE), a);
+                for (int e = 0; e < 4; ++e) a[e] = __fadd2_rn(a[e], *reinterpret_cast<const float2 *>(&part[q][lane * 8 + 2 * e]));
+            write(a, P.cuts[su].first_row, sl);
         }
         __syncthreads();
     }
@@ -580,18 +588,17 @@ tad_status tad_embed_backward(const void *tokens, int32_t token_bits, int64_t n_
     Sums P{};
     P.sorted = passes & 1 ? s0 : s1;
     P.dy = dy->data; P.dys = dy->stride;
-    P.dtable = dtable->data; P.ds = dtable->stride; P.type = dtable->type; P.accumulate = accumulate != 0;
+    P.dtable = dtable->data; P.ds = dtable->stride; P.accumulate = accumulate != 0;
     P.n = (unsigned)n_tokens; P.n_table = (unsigned)n_table; P.segments = l.segments; P.slices = l.slices; P.each = l.each;
     P.width = (int)width; P.factor = factor;
     P.head = reinterpret_cast<float *>(ws + 2 * l.sorted); P.tail = reinterpret_cast<float *>(ws + 2 * l.sorted + l.parts);
     P.cuts = reinterpret_cast<Cut *>(ws + 2 * l.sorted + 2 * l.parts);
     const bool eights = width % 8 == 0 && by_eights(dy) && by_eights(dtable);
     const unsigned grid = (unsigned)(((int64_t)l.segments * l.slices + NT / 32 - 1) / (NT / 32));
-    TAD_WITH_TYPE(dy->type, T, {
-        auto kernel = eights ? tad_embed_sums_kernel<T, 8> : tad_embed_sums_kernel<T, 1>;
-        e = tad_launch(kernel, grid, NT, 0, stream, P);
+    TAD_WITH_TYPE(dtable->type, O, {
+        TAD_WITH_TYPE(dy->type, T, e = tad_launch(eights ? tad_embed_sums_kernel<T, O, 8> : tad_embed_sums_kernel<T, O, 1>, grid, NT, 0, stream, P));
+        if (e == cudaSuccess && l.segments > 1) e = tad_launch(eights ? tad_embed_join_kernel<O, 8> : tad_embed_join_kernel<O, 1>, grid, NT, 0, stream, P);
     });
-    if (e == cudaSuccess && l.segments > 1) e = tad_launch(eights ? tad_embed_join_kernel<8> : tad_embed_join_kernel<1>, grid, NT, 0, stream, P);
     return launched("embedding gradient", e);
 }
 
