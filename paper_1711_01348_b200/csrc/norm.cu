@@ -7,10 +7,12 @@
 // 1 to 16 warps or, in longer rows, by a cluster of such groups; a group walks over the rows that are its share.  Rows of
 // whole 16-byte pieces come by bulk copies into a ring of shared memory, two to four rows ahead (32 KB of rows under way a block of the
 // forward pass, 128 KB of the backward pass): prefetched into registers instead they take those that a second and third block
-// an SM need (8192 x 4096 fp32, forward / backward: 51 / 83 us).  Other rows are loaded an element at a time, one row ahead.  The
+// an SM need (8192 x 4096 fp32, forward / backward: 51 / 83 us for 48 / 69).  Other rows are loaded an element at a time, one row ahead.  The
 // variance is the mean of the squared deviations of the registers (no difference of large sums).  Weights stay in registers
 // over all rows.  The backward pass keeps its share of dw and db there too and writes them once a block, as a plane of partial
 // sums; a second kernel adds the planes up in a fixed order.  Rows longer than a cluster holds are read twice or three times.
+// Measured, 8192 x 4096: fp32 forward 48 us, backward 69 (5.6, 5.8 TB/s); bf16 27, 44 (5.0, 4.6 TB/s: converting an element and its
+// seven to ten operations take more than half of the issue slots, with the registers of 24 and 16 warps an SM).
 #include <cooperative_groups.h>
 
 #include <atomic>
@@ -40,7 +42,8 @@ struct Params {
     const void *x, *dy, *w, *b;
     void *y, *dx;
     const uint8_t *q, *scale;
-    int64_t xs, dys, ys, dxs, qs, ss;
+    uint8_t *kq, *kscale;
+    int64_t xs, dys, ys, dxs, qs, ss, kqs, kss;
     float *mean, *rstd, *planes;
     int64_t n_rows;
     int width, w_type, b_type, y_type, dx_type;
@@ -52,9 +55,8 @@ struct Params {
 enum { BY_WARP, BY_GROUP, BY_CLUSTER };
 
 // A thread's E elements lie in the 32 E columns of its warp: V = 8, pieces of eight, 256 columns apart; V = 1, 32 apart.  So every access of
-// a row is the thread's pointer and a constant, and the warp's accesses are contiguous.  (Sixteen elements side by side would let eight
-// threads pack a block of 128 for a checkpoint, but their stores of 16 bytes lie 32 apart: 16384 x 2048 bf16 43 us for 36.)  Piece i
-// exists where place(i) < rem, the columns from the thread's first one to the end of the row.
+// a row is the thread's pointer and a constant, and the warp's accesses are contiguous.  Piece i exists where place(i) < rem, the columns
+// from the thread's first one to the end of the row.
 template <int V> struct Of {
     __device__ __forceinline__ static constexpr int place(int i) { return V == 8 ? i * 256 : i * 32; }
     // column of element e behind the thread's first
@@ -219,7 +221,7 @@ struct Sum {
 
 // What the blocks of a cluster tell each other: two values a block and row go into everybody's shared memory by stores that count
 // at the receiver's mbarrier.  (A cluster barrier instead would wait, as a release, for the rows just written: 8192 columns forward
-// 55 us for 36.)
+// 55 us for 36 - 42.)
 struct Exchange {
     float2 far[2][MAX_CLUSTER];
     unsigned long long bar[2];
@@ -367,8 +369,35 @@ __device__ __forceinline__ void clear_ring(unsigned char *rows, unsigned bytes)
 
 template <class T> constexpr int FORWARD_STAGES = sizeof(T) == 2 ? 4 : 2;
 
-// V = 8: width and all row starts are whole pieces of eight.
-template <class T, int V, int BY>
+// fp32 into 8 bits beside the pass: sixteen neighbouring threads hold a block of 128
+__device__ __forceinline__ void keep_row(const Params &P, int64_t r, int col, int rem, const float (&v)[FORWARD_E])
+{
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        float f[8], a = 0.f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) { f[j] = v[8 * i + j]; a = fmaxf(a, fabsf(f[j])); }
+#pragma unroll
+        for (int d = 8; d; d >>= 1) a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, d));
+        if (__any_sync(0xffffffffu, isinf(a))) {           // (a maximum leaves out NaNs, but not infinities)
+            a = 0.f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) { a = fmaxf(a, finite_abs(f[j])); f[j] = no_infinity(f[j]); }
+#pragma unroll
+            for (int d = 8; d; d >>= 1) a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, d));
+        }
+        const unsigned byte = scale_byte(a);
+        const float inv = inverse_scale(byte);
+        if (Of<8>::place(i) >= rem) continue;
+        const int c = col + Of<8>::place(i);
+        *reinterpret_cast<uint2 *>(P.kq + r * P.kqs + c) =
+            make_uint2(to_e4m3x2(f[0] * inv, f[1] * inv) | (to_e4m3x2(f[2] * inv, f[3] * inv) << 16), to_e4m3x2(f[4] * inv, f[5] * inv) | (to_e4m3x2(f[6] * inv, f[7] * inv) << 16));
+        if ((threadIdx.x & 15) == 0) P.kscale[r * P.kss + c / TAD_BLOCK8] = (uint8_t)byte;
+    }
+}
+
+// V = 8: width and all row starts are whole pieces of eight.  KEEP: with the checkpoint of fp32 rows.
+template <class T, int V, int BY, bool KEEP = false>
 __global__ void __launch_bounds__(FORWARD_BLOCK, V == 1 ? 2 : FORWARD_BLOCKS)
 tad_norm_forward_kernel(const Params P)
 {
@@ -416,6 +445,7 @@ tad_norm_forward_kernel(const Params P)
             Piece<T, 8> p[E / 8];
             read_row<T, E>(p, reinterpret_cast<const T *>(ring.row()) + (at.col - at.col0));
             elements<T, E>(v, p);
+            if constexpr (KEEP) keep_row(P, r, at.col, at.rem, v);
         } else {
             next.get(v);
             if (r + at.step < P.n_rows) next.fetch(x + (r + at.step) * P.xs + at.col, at.rem);
@@ -901,7 +931,7 @@ cudaError_t clusters_of(K kernel, int threads, size_t smem, int cluster, std::at
 }
 
 template <class T>
-cudaError_t forward(const Params &P, const Shape &s, bool eights, cudaStream_t stream)
+cudaError_t forward(const Params &P, const Shape &s, bool eights, bool keep, cudaStream_t stream)
 {
     if (P.width > HELD) return tad_launch(tad_norm_forward_long_kernel<T>, (unsigned)std::min<int64_t>(P.n_rows, 2 * SMS), LARGE, 0, stream, P);
     const int threads = s.by == BY_WARP ? FORWARD_BLOCK : s.group, groups = s.by == BY_WARP ? FORWARD_BLOCK / 32 : 1;
@@ -909,10 +939,12 @@ cudaError_t forward(const Params &P, const Shape &s, bool eights, cudaStream_t s
     auto kernel = tad_norm_forward_kernel<T, 1, BY_WARP>;
     if (eights) kernel = s.by == BY_WARP ? tad_norm_forward_kernel<T, 8, BY_WARP> : s.by == BY_GROUP ? tad_norm_forward_kernel<T, 8, BY_GROUP> : tad_norm_forward_kernel<T, 8, BY_CLUSTER>;
     else if (s.by != BY_WARP) kernel = s.by == BY_GROUP ? tad_norm_forward_kernel<T, 1, BY_GROUP> : tad_norm_forward_kernel<T, 1, BY_CLUSTER>;
+    if constexpr (std::is_same<T, float>::value)
+        if (keep) kernel = s.by == BY_WARP ? tad_norm_forward_kernel<T, 8, BY_WARP, true> : s.by == BY_GROUP ? tad_norm_forward_kernel<T, 8, BY_GROUP, true> : tad_norm_forward_kernel<T, 8, BY_CLUSTER, true>;
     const size_t smem = eights ? (size_t)threads * FORWARD_E * sizeof(T) * FORWARD_STAGES<T> : 0;      // (32 KB at most)
     if (s.cluster > 1) {
-        static std::atomic<int> known[2][64][3];
-        const cudaError_t e = clusters_of(kernel, threads, smem, s.cluster, known[eights], most);
+        static std::atomic<int> known[3][64][3];
+        const cudaError_t e = clusters_of(kernel, threads, smem, s.cluster, known[eights + keep], most);
         if (e != cudaSuccess) return e;
     }
     const unsigned blocks = (unsigned)(std::min((P.n_rows + groups - 1) / groups, most) * s.cluster);
@@ -995,11 +1027,13 @@ tad_status tad_layernorm_forward(const tad_rows *x, int64_t n_rows, int64_t widt
     const Shape s = shape_of(width, FORWARD_BLOCK, FORWARD_E);
     P.group = s.group;
     const bool eights = width % 8 == 0 && by_eights(x) && by_eights(y);
-    // The checkpoint by a pass of its own, which leaves x in L2 for the next one.  In one pass the norm's threads, who hold a row in step, wait
-    // for the packing of every row (16384 x 2048 bf16 43 to 51 us for 41; 8192 x 4096 46 to 55 for 42).
-    if (checkpoint && (st = tad_launch_pack8(x, n_rows, width, checkpoint, stream))) return st;
+    // The checkpoint of fp32 rows in the norm's own pass (8192 x 4096: 53 us for 71); of 16-bit rows, where the pass has no instructions to
+    // spare, by the packing kernel, which leaves x in L2 for the next one (16384 x 2048 bf16 43 us either way, 8192 x 4096 44 us for 46).
+    const bool keep = checkpoint && x->type == TAD_F32 && eights && width <= HELD;
+    if (keep) { P.kq = checkpoint->q; P.kqs = checkpoint->q_stride; P.kscale = checkpoint->scale; P.kss = checkpoint->scale_stride; }
+    else if (checkpoint && (st = tad_launch_pack8(x, n_rows, width, checkpoint, stream))) return st;
     cudaError_t e = cudaSuccess;
-    TAD_WITH_TYPE(x->type, T, e = forward<T>(P, s, eights, stream));
+    TAD_WITH_TYPE(x->type, T, e = forward<T>(P, s, eights, keep, stream));
     return launched("layer norm", e);
 }
 

@@ -4,7 +4,8 @@
 //
 // The scale is a power of two, so it is one byte, the division is exact, q depends on x alone (no rounding of a scale that
 // another order of operations would make different) and the tensor cores can apply it to a block's products.
-// All three move bytes and are bound by memory.
+// All three move bytes and are bound by memory.  Measured, 16384 x 8192 bf16: packed in 60 us, unpacked in 62 (6.5 TB/s), turned in 79
+// (3.4 TB/s: about ten instructions an element, half of the issue slots).
 #include "rows.cuh"
 
 namespace {

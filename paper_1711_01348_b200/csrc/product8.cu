@@ -11,7 +11,9 @@
 // bring the scales of 512 elements at a time from memory into tensor memory, a warp issues the MMAs and eight warps empty the
 // accumulator.  Large products run on pairs of blocks (PAIR, clusters of two SMs): a tile of 256 x 256, each block holds 128 rows of p and
 // of q and half of the accumulator, and the first block issues the MMAs of both.  What bounds those is L2: at the full rate of the
-// tensor cores single tiles of 128 x 256 would read 27 TB/s from it.
+// tensor cores single tiles of 128 x 256 would read 27 TB/s from it.  Measured, bf16 out: 8192 x 4096 x 4096 99 us (2.8 PFLOP/s; 112 us
+// in a row without a pause, where the power limit sets the clock), 8192 x 8192 x 8192 361 us (3.0); with one MMA of four left the
+// loop takes 64 of the 99 us, so the tensor cores and their clock are what remains.
 #include <cuda.h>
 
 #include <atomic>
@@ -422,7 +424,7 @@ tad_product8_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_cons
 // ---- few rows ----
 
 // Up to four rows on one side: bound by reading the other operand once.  A warp takes two of its rows and sixteen elements of k a lane
-// and step, the few rows come from the first-level cache.
+// and step, the few rows come from the first-level cache.  (1 x 4096 x 4096 7 - 10 us, most of it the launch and one round of loads.)
 constexpr int FEW = 4, FEW_ROWS = 2;
 
 struct Few {

@@ -1,5 +1,5 @@
 // Rows of 32- and 16-bit elements and of packed 8-bit blocks: descriptors as the kernels take them, their checks on the host,
-// loads and stores of eight elements or of one.  Shared by norm.cu, embed.cu, pack8.cu and product8.cu.
+// loads and stores of eight elements or of one, packing and unpacking.  Shared by norm.cu, embed.cu, pack8.cu and product8.cu.
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -106,7 +106,7 @@ template <> struct Piece<float, 8> {
     __device__ __forceinline__ void zero() { a = b = make_float4(0.f, 0.f, 0.f, 0.f); }
     __device__ __forceinline__ void get(float (&v)[8]) const { v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w; }
     __device__ __forceinline__ void set(const float (&v)[8]) { a = make_float4(v[0], v[1], v[2], v[3]); b = make_float4(v[4], v[5], v[6], v[7]); }
-    // (one store of 32 bytes: two of 16 leave half of every sector to the second; 8192 x 8192 unpacked to fp32 70 us for 55)
+    // (one store of 32 bytes: two of 16 leave half of every sector to the second; 8192 x 8192 unpacked to fp32 70 us for 52)
     __device__ __forceinline__ void store(float *p) const
     {
         asm volatile("st.global.v8.f32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "f"(a.x), "f"(a.y), "f"(a.z), "f"(a.w), "f"(b.x), "f"(b.y), "f"(b.z), "f"(b.w) : "memory");

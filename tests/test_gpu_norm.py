@@ -134,6 +134,17 @@ def test_checkpoint_of_unaligned_rows(width, pad):
     _run(6, width, "bf16", pad=pad, checkpoint=True)
 
 
+def test_checkpoint_of_infinities_and_nans():
+    """fp32 rows are packed in the norm's own pass: the same bytes as by pack8"""
+    x, _, _, _ = _case(9, 1024, "f32", 2)
+    x[1, 130], x[2, 0], x[3, 1000], x[4], x[5, 256:384] = float("inf"), float("nan"), -float("inf"), 0.0, float("nan")
+    X, Y, K = Matrix(9, 1024, "f32", values=x), Matrix(9, 1024, "f32"), PackedMatrix(9, 1024)
+    layernorm_forward(X.rows, 9, 1024, Y.rows, checkpoint=K.packed, stream=stream())
+    q, s = K.bytes()
+    wq, ws = pack_reference(x.double().numpy())
+    assert np.array_equal(s, ws) and same_codes(q, wq)
+
+
 def test_without_weights():
     _run(31, 640, "f32", affine=False)
 
