@@ -423,9 +423,12 @@ tad_product8_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_cons
 
 // ---- few rows ----
 
-// Up to four rows on one side: bound by reading the other operand once.  A warp takes two of its rows and sixteen elements of k a lane
-// and step, the few rows come from the first-level cache.  (1 x 4096 x 4096 7 - 10 us, most of it the launch and one round of loads.)
+// Up to four rows on one side and little work: bound by its launch and one round of loads.  A warp takes two rows of the other operand and
+// sixteen elements of k a lane and step, the few rows come from the first-level cache.  Four instructions an element and row make it
+// slower than the tensor cores from some 20 million multiply-adds on; us, these / those: 1 x 256 x 256 2.0 / 4.4, 4 x 1000 x 1000 4.3 / 5.8,
+// 1 x 4096 x 4096 6.3 / 7.5, 2 x 4096 x 4096 8.9 / 7.5, 1 x 65536 x 512 15 / 11, 1 x 16384 x 8192 35 / 27.
 constexpr int FEW = 4, FEW_ROWS = 2;
+constexpr int64_t FEW_WORK = int64_t(20) << 20;
 
 struct Few {
     const uint8_t *q, *s, *fq, *fs;                // the many rows, the few rows
@@ -469,7 +472,10 @@ tad_product8_few_kernel(const Few P)
             unpack_eight(make_uint2(u.x, u.y), s, lo);
             unpack_eight(make_uint2(u.z, u.w), s, hi);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) { x[f][j] = j < left ? lo[j] : 0.f; x[f][8 + j] = 8 + j < left ? hi[j] : 0.f; }
+            for (int j = 0; j < 8; ++j) { x[f][j] = lo[j]; x[f][8 + j] = hi[j]; }
+            if (left < 16)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) if (j >= left) x[f][j] = 0.f;
         }
 #pragma unroll
         for (int i = 0; i < FEW_ROWS; ++i) {
@@ -477,13 +483,16 @@ tad_product8_few_kernel(const Few P)
             unpack_eight(make_uint2(w[i].x, w[i].y), 1.f, lo);
             unpack_eight(make_uint2(w[i].z, w[i].w), 1.f, hi);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) { v[j] = j < left ? lo[j] : 0.f; v[8 + j] = 8 + j < left ? hi[j] : 0.f; }
+            for (int j = 0; j < 8; ++j) { v[j] = lo[j]; v[8 + j] = hi[j]; }
+            if (left < 16)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) if (j >= left) v[j] = 0.f;
 #pragma unroll
             for (int f = 0; f < F; ++f) {
-                float d = 0.f;
+                float2 d = make_float2(0.f, 0.f);
 #pragma unroll
-                for (int j = 0; j < 16; ++j) d = fmaf(v[j], x[f][j], d);
-                acc[i][f] = fmaf(d, ws[i], acc[i][f]);
+                for (int j = 0; j < 16; j += 2) d = __ffma2_rn(make_float2(v[j], v[j + 1]), make_float2(x[f][j], x[f][j + 1]), d);
+                acc[i][f] = fmaf(d.x + d.y, ws[i], acc[i][f]);
             }
         }
     }
@@ -534,7 +543,7 @@ Way way_of(int64_t m, int64_t n, int64_t k)
     Way w{};
     const int64_t s = std::min(m, n);
     w.blocks = (int)blocks_of(k);
-    w.few = s <= FEW;
+    w.few = s <= FEW && s * std::max(m, n) * k <= FEW_WORK;
     w.split = 1;
     w.p_is_b = s <= 128 && n > m;
     if (w.few) return w;

@@ -54,7 +54,7 @@ def test_one_side_short(m, n, k):
     _check(m, n, k)
 
 
-@pytest.mark.parametrize("m,n,k", [(1, 1, 1), (1, 4096, 4096), (2, 33, 15), (3, 100, 1000), (4, 555, 513), (1000, 1, 777), (77, 3, 4097), (4, 4, 20000), (1, 3, 16)])
+@pytest.mark.parametrize("m,n,k", [(1, 1, 1), (1, 4096, 4096), (2, 4096, 4096), (3, 1000, 7001), (1, 30000, 800), (2, 33, 15), (3, 100, 1000), (4, 555, 513), (1000, 1, 777), (77, 3, 4097), (4, 4, 20000), (1, 3, 16)])
 def test_few_rows(m, n, k):
     _check(m, n, k)
 
