@@ -904,8 +904,8 @@ int64_t planes_of(int64_t n_rows, int64_t width, int e)
 }
 
 // Clusters that run at a time: not all SMs of the device have enough neighbours, and one that has to wait for another doubles the time
-// (2048 x 16384 bf16 forward 72 us for 49).  The device is asked once for a kernel and a size of clusters; `known`: 64 devices,
-// clusters of 2, 4 and 8.
+// (2048 x 16384 bf16 forward 72 us for 49).  The device is asked once for a kernel, its threads and a size of clusters; `known`:
+// 64 devices, clusters of 2, 4 and 8.
 template <class K>
 cudaError_t clusters_of(K kernel, int threads, size_t smem, int cluster, std::atomic<int> (*known)[3], int64_t &most)
 {
@@ -986,9 +986,9 @@ cudaError_t backward(Params &P, bool eights, int64_t &planes, cudaStream_t strea
         smem = (size_t)threads * BACKWARD_E<8> * (SOURCE_BYTES<S> + sizeof(T)) * BACKWARD_STAGES<S, T>;
     }
     if (s.cluster > 1) {
-        static std::atomic<int> known[2][64][3];
+        static std::atomic<int> known[2][2][64][3];                          // (by the kernel and its threads)
         int64_t most = 0;
-        const cudaError_t e = clusters_of(kernel, threads, smem, s.cluster, known[eights], most);
+        const cudaError_t e = clusters_of(kernel, threads, smem, s.cluster, known[eights][threads == BACKWARD_BLOCK], most);
         if (e != cudaSuccess) return e;
         planes = std::min(planes, most);
     }
@@ -1076,7 +1076,7 @@ tad_status tad_layernorm_backward(const tad_rows *dy, const tad_rows *x, const t
         P.mean = const_cast<float *>(mean); P.rstd = const_cast<float *>(rstd);
         P.planes = sums ? static_cast<float *>(workspace) : nullptr;
         P.n_rows = n_rows; P.width = (int)width; P.inv_width = 1.f / (float)width;
-                const bool eights = width % 8 == 0 && by_eights(dy) && (!x || by_eights(x)) && (!dx || by_eights(dx));
+        const bool eights = width % 8 == 0 && by_eights(dy) && (!x || by_eights(x)) && (!dx || by_eights(dx));
         TAD_WITH_TYPE(dy->type, T, {
             if (!x) e = backward<Packed8, T>(P, eights, planes, stream);
             else TAD_WITH_TYPE(x->type, S, e = (backward<S, T>(P, eights, planes, stream)));

@@ -54,3 +54,32 @@ print("same")
 def test_first_calls_captured():
     r = subprocess.run([sys.executable, "-c", SCRIPT], capture_output=True, text=True, timeout=300)
     assert r.returncode == 0 and r.stdout.strip().endswith("same"), r.stdout + r.stderr
+
+
+ORDER = """
+import os, sys
+sys.path.insert(0, os.getcwd())
+import torch
+import paper_1711_01348_b200 as tad
+def backward(n, d):
+    torch.manual_seed(d)
+    x, dy, dx, dw = (torch.randn((k, d), device="cuda").bfloat16() for k in (n, n, n, 1))
+    mean, rstd, dw = torch.zeros(n, device="cuda"), torch.ones(n, device="cuda"), dw.float()
+    need = tad.layernorm_workspace_bytes(n, d)
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    rows = lambda t, kind: tad.Rows(t.data_ptr(), t.stride(0), kind)
+    tad.layernorm_backward(rows(dy, "bf16"), rows(x, "bf16"), None, n, d, mean.data_ptr(), rstd.data_ptr(), rows(dx, "bf16"), dweight=rows(dw, "f32"),
+                           workspace_ptr=ws.data_ptr(), workspace_bytes=need, stream=torch.cuda.current_stream().cuda_stream)
+    return dx, dw
+import hashlib
+for d in map(int, sys.argv[1:]): last = backward(200, d)
+print(hashlib.sha256(b"".join(t.contiguous().view(torch.uint8).cpu().numpy().tobytes() for t in last)).hexdigest())
+"""
+
+
+def test_earlier_calls_change_nothing():
+    """widths whose rows take clusters of the same size, of blocks of 256 and of 512 threads: the number of partial sums of one does not
+    depend on whether the other came before"""
+    out = [subprocess.run([sys.executable, "-c", ORDER, *widths], capture_output=True, text=True, timeout=300) for widths in (("12001",), ("20001", "12001"))]
+    assert all(r.returncode == 0 for r in out), out[0].stderr + out[1].stderr
+    assert out[0].stdout.split() == out[1].stdout.split() != []
