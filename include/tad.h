@@ -334,7 +334,7 @@ tad_status tad_repack8(const tad_packed *in, int64_t n_rows, int64_t width, cons
  * tad_layernorm_forward:  y = (x - mean) rstd weight + bias  over each row, mean = sum x / width,
  * rstd = 1 / sqrt(sum (x - mean)^2 / width + eps), statistics in fp32.
  *   weight, bias   vectors of `width` elements; NULL = ones, zeros
- *   mean, rstd     n_rows floats each, what the backward pass needs; NULL = not wanted
+ *   mean, rstd     n_rows floats each, what the backward pass needs; NULL = not wanted (and refused where width = 0: there is no mean)
  *   checkpoint     NULL, or x in 8 bits exactly as tad_pack8 gives it
  * y may have another type than x.
  * tad_layernorm_backward:  with xh = (x - mean) rstd and g = dy weight,

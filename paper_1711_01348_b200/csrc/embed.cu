@@ -504,13 +504,14 @@ tad_status check_tokens(const char *what, const void *tokens, int32_t bits, int6
     return TAD_OK;
 }
 
+int64_t odd_chunks(int64_t width) { return (width + 32 * ODD - 1) / (32 * ODD); }
+
 template <class S, class T>
 cudaError_t embed_forward(const Tokens &tok, int64_t n, const tad_rows *table, int64_t width, float factor, const tad_rows *y, cudaStream_t stream)
 {
     const bool eights = width % 8 == 0 && by_eights(table) && by_eights(y);
     if (!eights) {
-        const int64_t chunks = (width + 32 * ODD - 1) / (32 * ODD), blocks = (n * chunks + NT / 32 - 1) / (NT / 32);
-        if (blocks >= MAX_ROWS) return cudaErrorInvalidValue;
+        const int64_t chunks = odd_chunks(width), blocks = (n * chunks + NT / 32 - 1) / (NT / 32);
         return tad_launch(tad_embed_forward_odd_kernel<S, T>, (unsigned)blocks, NT, 0, stream, tok, n, static_cast<const S *>(table->data), table->stride, (int)width, factor,
                           static_cast<T *>(y->data), y->stride, (unsigned)chunks);
     }
@@ -518,7 +519,6 @@ cudaError_t embed_forward(const Tokens &tok, int64_t n, const tad_rows *table, i
     int log = 0;
     while (log < 8 && (int64_t(1) << log) < pieces) ++log;
     const int64_t chunks = (pieces + (1 << log) - 1) >> log, rows = ROWS * (NT >> log), blocks = (n + rows - 1) / rows * chunks;
-    if (blocks >= MAX_ROWS) return cudaErrorInvalidValue;
     return tad_launch(tad_embed_forward_kernel<S, T>, (unsigned)blocks, NT, 0, stream, tok, n, static_cast<const S *>(table->data), table->stride, (int)width, factor,
                       static_cast<T *>(y->data), y->stride, log, (unsigned)chunks);
 }
@@ -534,6 +534,8 @@ tad_status tad_embed_forward(const void *tokens, int32_t token_bits, int64_t n_t
     if ((st = check_sizes("embed_forward", n_tokens, width)) || (st = check_tokens("embed_forward", tokens, token_bits, n_tokens, n_table)) ||
         (st = check_rows("embed_forward: table", table, n_table, width)) || (st = check_rows("embed_forward: y", y, n_tokens, width))) return st;
     if (n_tokens == 0 || width == 0) return TAD_OK;
+    // more blocks than a launch has, in either form (of matrices beyond any memory)
+    if (n_tokens * odd_chunks(width) >= MAX_ROWS * (NT / 32) - NT) { tad::set_error("embed_forward: too many blocks"); return TAD_ERR_UNSUPPORTED; }
     const Tokens tok{tokens, token_bits, (unsigned)n_table};
     cudaError_t e = cudaSuccess;
     TAD_WITH_TYPE(table->type, S, TAD_WITH_TYPE(y->type, T, e = (embed_forward<S, T>(tok, n_tokens, table, width, factor, y, (cudaStream_t)cuda_stream))));

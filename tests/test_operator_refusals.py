@@ -167,6 +167,13 @@ def test_good_calls_reach_the_launch():
         _refused(call, "TAD_ERR_CUDA")
 
 
+@fake
+def test_lookups_beyond_a_launch():
+    for offset in (0, 4):
+        m = Rows(P + offset, 1 << 40, "f32")
+        _refused(lambda: embed_forward(P, 32, (1 << 31) - 1, m, 7, (1 << 24) - 8, 1.0, m), "TAD_ERR_UNSUPPORTED")
+
+
 def test_descriptors_have_the_layout_of_the_header():
     assert C.sizeof(Rows) == 24 and Rows.stride.offset == 8 and Rows.type.offset == 16
     assert C.sizeof(Packed) == 32 and Packed.q_stride.offset == 16 and Packed.scale_stride.offset == 24
