@@ -201,20 +201,17 @@ struct Sum {
         // (barriers with a number known at run time only count as all sixteen of a block: four blocks an SM)
         if (ALONE) __syncthreads();
         else asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
-#pragma unroll
-        for (int k = 0; k < N; ++k) v[k] = 0.f;
+        float2 both = make_float2(0.f, 0.f);                       // N = 2: the two sums; N = 1: of the even and of the odd warps
 #pragma unroll
         for (int w = 0; w < BACKWARD_BLOCK / 32; w += 2) {         // (groups have an even number of warps)
             if (w >= warps) break;
             if (N == 2) {
                 const float4 p = *reinterpret_cast<const float4 *>(&box[turn][first + w][0]);
-                v[0] += p.x + p.z;
-                v[N - 1] += p.y + p.w;
-            } else {
-                const float2 p = *reinterpret_cast<const float2 *>(&box[turn][first + w][0]);
-                v[0] += p.x + p.y;
-            }
+                both = __fadd2_rn(both, __fadd2_rn(make_float2(p.x, p.y), make_float2(p.z, p.w)));
+            } else both = __fadd2_rn(both, *reinterpret_cast<const float2 *>(&box[turn][first + w][0]));
         }
+        if (N == 2) { v[0] = both.x; v[N - 1] = both.y; }
+        else v[0] = both.x + both.y;
         turn ^= 1;
     }
 };
@@ -329,6 +326,13 @@ struct Ring {
     {
         if (bytes) asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_u32(rows) + buf + i * stage_bytes + offset), "l"(from), "r"(bytes), "r"(bars + 8 * i) : "memory");
     }
+    // by the threads of the group: zeros into the bytes of every stage that no copy writes; a barrier follows
+    __device__ __forceinline__ void zeros(unsigned from, unsigned to, int in, int threads) const
+    {
+        for (unsigned b = from + in * 16; b < to; b += threads * 16)
+#pragma unroll
+            for (int i = 0; i < STAGES; ++i) *reinterpret_cast<uint4 *>(rows + buf + i * stage_bytes + b) = make_uint4(0, 0, 0, 0);
+    }
     // waits for the row at the ring's head (a second at most)
     __device__ __forceinline__ bool wait()
     {
@@ -340,7 +344,7 @@ struct Ring {
 };
 
 // The thread's elements of a row in the ring.  Every thread reads its places, whether they exist or not: those behind the row hold zeros
-// from the start (clear_ring), which costs no selects where the row is read.
+// from the start (Ring::zeros), which costs no selects where the row is read.
 template <class T, int E>
 __device__ __forceinline__ void read_row(Piece<T, 8> (&p)[E / 8], const T *at)
 {
@@ -358,13 +362,6 @@ __device__ __forceinline__ void elements(float (&v)[E], const Piece<T, 8> (&p)[E
         for (int j = 0; j < 8; ++j) v[i * 8 + j] = f[j];
     }
 }
-// by the whole block, before the first copy; a barrier follows
-__device__ __forceinline__ void clear_ring(unsigned char *rows, unsigned bytes)
-{
-    for (unsigned i = threadIdx.x * 16; i < bytes; i += blockDim.x * 16) *reinterpret_cast<uint4 *>(rows + i) = make_uint4(0, 0, 0, 0);
-    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");             // (the copies write the same places)
-}
-
 // ---- forward ----
 
 template <class T> constexpr int FORWARD_STAGES = sizeof(T) == 2 ? 4 : 2;
@@ -408,24 +405,23 @@ tad_norm_forward_kernel(const Params P)
     extern __shared__ __align__(128) unsigned char rows[];
     tad_wait_previous();
     Sum<1, BY, true> sum = sum_of<1, BY, true>(P, box);
-    Trade trade;
-    if constexpr (BY == BY_CLUSTER) trade.start(&ex);
     const Place<BY, V, E> at(P);
     int64_t r = at.row;
     const T *__restrict__ x = static_cast<const T *>(P.x);
     Held<T, 1, V == 1 ? E : 1> next;       // (V = 1)
     Ring<STAGES> ring;
     const unsigned columns = (unsigned)max(0, min(P.width - at.col0, P.group * E)), bytes = columns * (unsigned)sizeof(T);
+    // the first rows are under way before anything else is done
     if constexpr (V != 1) {
-        ring.start(rows, at.group * STAGES * P.group * E * (unsigned)sizeof(T), smem_u32(&bars[at.group][0]), P.group * E * (unsigned)sizeof(T), at.in == 0);
-        clear_ring(rows, blockDim.x * STAGES * E * (unsigned)sizeof(T));
-        __syncthreads();
+        const unsigned stage = P.group * E * (unsigned)sizeof(T);
+        ring.start(rows, at.group * STAGES * stage, smem_u32(&bars[at.group][0]), stage, at.in == 0);
         if (ring.leader)
             for (int i = 0; i < STAGES; ++i)
                 if (r + i * at.step < P.n_rows) {
                     ring.expect(i, bytes);
                     ring.copy(i, 0, x + (r + i * at.step) * P.xs + at.col0, bytes);
                 }
+        ring.zeros(bytes, stage, at.in, P.group);
     } else {
         next.zero();
         if (r < P.n_rows) next.fetch(x + r * P.xs + at.col, at.rem);
@@ -438,6 +434,9 @@ tad_norm_forward_kernel(const Params P)
         load_vector<V, E>(f, P.b, P.b_type, at.col, at.rem, 0.f);
         b.set(f);
     }
+    Trade trade;
+    if constexpr (BY == BY_CLUSTER) trade.start(&ex);
+    else if constexpr (V != 1) __syncthreads();
     for (; r < P.n_rows; r += at.step) {
         float v[E];
         if constexpr (V != 1) {
@@ -608,6 +607,50 @@ template <class S> constexpr int SOURCE_BYTES = sizeof(S);
 template <> constexpr int SOURCE_BYTES<Packed8> = 1;
 template <class S, class T> constexpr int BACKWARD_STAGES = SOURCE_BYTES<S> + (int)sizeof(T) <= 4 ? 4 : 2;
 
+// The block's plane (group, t, col: a thread's place): its groups are added up in order through shared memory, all elements at once (V = 8 in the ring, which nobody reads
+// any more), every thread's next to its neighbour's.  (Eight elements at a time, a thread's in a row: 3.3 us for 1.)
+template <int V, int E>
+__device__ __forceinline__ void join_groups(const Params &P, const float (&dw)[E], const float (&db)[E], float *room, int group, int t, int col)
+{
+    float *plane = P.planes + (size_t)blockIdx.x * 2 * P.width;
+    const int groups = blockDim.x / P.group;
+    __syncthreads();
+    if constexpr (V == 8) {
+        float4 *to = reinterpret_cast<float4 *>(room);
+#pragma unroll
+        for (int q = 0; q < E / 4; ++q) {
+            to[q * blockDim.x + threadIdx.x] = make_float4(dw[4 * q], dw[4 * q + 1], dw[4 * q + 2], dw[4 * q + 3]);
+            to[(E / 4 + q) * blockDim.x + threadIdx.x] = make_float4(db[4 * q], db[4 * q + 1], db[4 * q + 2], db[4 * q + 3]);
+        }
+        __syncthreads();
+        for (int p = group; p < E / 4; p += groups) {
+            const int c = col + Of<8>::place(p % (E / 8));
+            if (c >= P.width) break;
+            float a[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+            for (int g = 0; g < groups; ++g) {
+                const float4 x = to[2 * p * blockDim.x + g * P.group + t], y = to[(2 * p + 1) * blockDim.x + g * P.group + t];
+                a[0] += x.x; a[1] += x.y; a[2] += x.z; a[3] += x.w; a[4] += y.x; a[5] += y.y; a[6] += y.z; a[7] += y.w;
+            }
+            Piece<float, 8> o;
+            o.set(a);
+            o.store(plane + (p < E / 8 ? 0 : (size_t)P.width) + c);
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            room[e * blockDim.x + threadIdx.x] = dw[e];
+            room[(E + e) * blockDim.x + threadIdx.x] = db[e];
+        }
+        __syncthreads();
+        for (int p = group; p < 2 * E; p += groups) {
+            const int c = col + Of<1>::place(p % E);
+            float a = 0.f;
+            for (int g = 0; g < groups; ++g) a += room[p * blockDim.x + g * P.group + t];
+            if (c < P.width) plane[(p < E ? 0 : (size_t)P.width) + c] = a;
+        }
+    }
+}
+
 template <class S, class T, int V, int BY>
 __global__ void __launch_bounds__(BACKWARD_BLOCK, 1)
 tad_norm_backward_kernel(const Params P)
@@ -617,11 +660,9 @@ tad_norm_backward_kernel(const Params P)
     __shared__ Exchange ex;
     __shared__ unsigned long long bars[BACKWARD_BLOCK / 32][STAGES];
     extern __shared__ __align__(128) unsigned char rows[];
-    __shared__ __align__(16) float join[BY == BY_CLUSTER ? 1 : BACKWARD_BLOCK][BY == BY_CLUSTER ? 4 : 8];
+    __shared__ __align__(16) float join[V == 8 || BY == BY_CLUSTER ? 1 : 2 * E * BACKWARD_BLOCK];
     tad_wait_previous();
     Sum<2, BY, BY == BY_CLUSTER> sum = sum_of<2, BY, BY == BY_CLUSTER>(P, box);
-    Trade trade;
-    if constexpr (BY == BY_CLUSTER) trade.start(&ex);
     const Place<BY, V, E> at(P);
     int64_t r = at.row;
     const T *__restrict__ dy = static_cast<const T *>(P.dy);
@@ -653,13 +694,14 @@ tad_norm_backward_kernel(const Params P)
             for (int i = 0; i < E / 8; ++i) if (Of<8>::place(i) < at.rem) nscale[i] = P.scale[row * P.ss + (at.col + Of<8>::place(i)) / TAD_BLOCK8];
         }
     };
+    // the first rows are under way before anything else is done
     if constexpr (V == 8) {
         const unsigned stage = held * (SOURCE_BYTES<S> + (unsigned)sizeof(T));
         ring.start(rows, at.group * STAGES * stage, smem_u32(&bars[at.group][0]), stage, at.in == 0);
-        clear_ring(rows, blockDim.x * STAGES * E * (SOURCE_BYTES<S> + (unsigned)sizeof(T)));
-        __syncthreads();
         if (ring.leader)
             for (int i = 0; i < STAGES; ++i) if (r + i * at.step < P.n_rows) issue(i, r + i * at.step);
+        ring.zeros(x_bytes, held * SOURCE_BYTES<S>, at.in, P.group);
+        ring.zeros(held * SOURCE_BYTES<S> + dy_bytes, stage, at.in, P.group);
 #pragma unroll
         for (int i = 0; i < E / 8; ++i) nscale[i] = 127;
     } else {
@@ -673,10 +715,13 @@ tad_norm_backward_kernel(const Params P)
         load_vector<V, E>(f, P.w, P.w_type, at.col, at.rem, 1.f);
         w.set(f);
     }
+    Trade trade;
+    if constexpr (BY == BY_CLUSTER) trade.start(&ex);
+    else if constexpr (V == 8) __syncthreads();
 #pragma unroll
     for (int j = 0; j < E / 2; ++j) dws.p[j] = dbs.p[j] = make_float2(0.f, 0.f);
     for (; r < P.n_rows; r += at.step) {
-        float xh[E], d[E];
+        float xh[E], d[E], xscale[E / 8];
         const float mean = nmean;
         float rstd = nrstd;
         if constexpr (V == 8) {
@@ -689,7 +734,8 @@ tad_norm_backward_kernel(const Params P)
                     uint2 q = *reinterpret_cast<const uint2 *>(from + c + Of<8>::place(i));
                     if (Of<8>::place(i) >= at.rem) q = make_uint2(0, 0);     // (copies end on whole sixteens, eight bytes behind the row at most)
                     float f[8];
-                    unpack_eight(q, scale_of(nscale[i]), f);
+                    unpack_eight(q, 1.f, f);
+                    xscale[i] = scale_of(nscale[i]);
 #pragma unroll
                     for (int j = 0; j < 8; ++j) xh[i * 8 + j] = f[j];
                 }
@@ -707,19 +753,23 @@ tad_norm_backward_kernel(const Params P)
         }
         fetch(r + at.step);
         if (V == 8 && ring.lost) rstd = __uint_as_float(0x7fffffffu);        // (a row that never came has no result)
-        Pairs<E> h, g;
+        Pairs<E> h, dp;
         h.set(xh);
-        g.set(d);
+        dp.set(d);
         float2 s1 = make_float2(0.f, 0.f), s2 = s1;
 #pragma unroll
         for (int j = 0; j < E / 2; ++j) {
             // behind the row xh is zero: zero times an infinite rstd or a NaN mean would reach the sums
-            h.p[j] = __fmul2_rn(__fadd2_rn(h.p[j], inside<V>(-mean, j, at.rem)), inside<V>(rstd, j, at.rem));
-            dws.p[j] = __ffma2_rn(g.p[j], h.p[j], dws.p[j]);
-            dbs.p[j] = __fadd2_rn(dbs.p[j], g.p[j]);
-            g.p[j] = __fmul2_rn(g.p[j], w.p[j]);
-            s1 = __fadd2_rn(s1, g.p[j]);
-            s2 = __ffma2_rn(g.p[j], h.p[j], s2);
+            const float2 shift = inside<V>(-mean, j, at.rem);
+            // (a packed value times its scale is exact)
+            if constexpr (PACKED && V == 8) h.p[j] = __ffma2_rn(h.p[j], make_float2(xscale[j / 4], xscale[j / 4]), shift);
+            else h.p[j] = __fadd2_rn(h.p[j], shift);
+            h.p[j] = __fmul2_rn(h.p[j], inside<V>(rstd, j, at.rem));
+            dws.p[j] = __ffma2_rn(dp.p[j], h.p[j], dws.p[j]);
+            dbs.p[j] = __fadd2_rn(dbs.p[j], dp.p[j]);
+            const float2 g = __fmul2_rn(dp.p[j], w.p[j]);
+            s1 = __fadd2_rn(s1, g);
+            s2 = __ffma2_rn(g, h.p[j], s2);
         }
         float s[2] = {s1.x + s1.y, s2.x + s2.y};
         sum.of(s);
@@ -737,8 +787,8 @@ tad_norm_backward_kernel(const Params P)
             const float c1 = -s[0] * P.inv_width, c2 = -s[1] * P.inv_width;
             const float2 rr = make_float2(rstd, rstd), m1 = make_float2(c1, c1), m2 = make_float2(c2, c2);
 #pragma unroll
-            for (int j = 0; j < E / 2; ++j) g.p[j] = __fmul2_rn(rr, __ffma2_rn(h.p[j], m2, __fadd2_rn(g.p[j], m1)));
-            g.get(d);
+            for (int j = 0; j < E / 2; ++j) dp.p[j] = __fmul2_rn(rr, __ffma2_rn(h.p[j], m2, __ffma2_rn(dp.p[j], w.p[j], m1)));
+            dp.get(d);
             store_typed<V, E>(P.dx, P.dx_type, r * P.dxs + at.col, at.rem, d);
         }
     }
@@ -757,23 +807,7 @@ tad_norm_backward_kernel(const Params P)
                 plane[(size_t)P.width + Of<V>::column(e)] = db[e];
             }
     } else {
-        // the groups of the block are added up in order, eight elements of every thread at a time
-        float *plane = P.planes + (size_t)blockIdx.x * 2 * P.width;
-        const int groups = blockDim.x / P.group;
-#pragma unroll
-        for (int part = 0; part < E / 4; ++part) {
-            __syncthreads();
-#pragma unroll
-            for (int k = 0; k < 8; ++k) join[threadIdx.x][k] = part < E / 8 ? dw[part % (E / 8) * 8 + k] : db[part % (E / 8) * 8 + k];
-            __syncthreads();
-            for (int u = threadIdx.x; u < P.group * 8; u += blockDim.x) {
-                const int t = u >> 3, e = part % (E / 8) * 8 + (u & 7);
-                const int c = (t >> 5) * (32 * E) + (t & 31) * V + Of<V>::column(e);
-                float a = 0.f;
-                for (int g = 0; g < groups; ++g) a += join[g * P.group + t][u & 7];
-                if (c < P.width) plane[(part < E / 8 ? 0 : (size_t)P.width) + c] = a;
-            }
-        }
+        join_groups<V, E>(P, dw, db, V == 8 ? reinterpret_cast<float *>(rows) : join, at.group, at.in, at.col);
     }
 }
 
