@@ -625,7 +625,7 @@ __device__ __forceinline__ void join_groups(const Params &P, const float (&dw)[E
         __syncthreads();
         for (int p = group; p < E / 4; p += groups) {
             const int c = col + Of<8>::place(p % (E / 8));
-            if (c >= P.width) break;
+            if (c >= P.width) continue;
             float a[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
             for (int g = 0; g < groups; ++g) {
                 const float4 x = to[2 * p * blockDim.x + g * P.group + t], y = to[(2 * p + 1) * blockDim.x + g * P.group + t];
