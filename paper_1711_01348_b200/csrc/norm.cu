@@ -964,12 +964,19 @@ cudaError_t clusters_of(K kernel, int threads, size_t smem, int cluster, std::at
     return cudaSuccess;
 }
 
+constexpr int64_t EVEN_BYTES = 96000000;
+constexpr int EVEN = 5;
+
 template <class T>
 cudaError_t forward(const Params &P, const Shape &s, bool eights, bool keep, cudaStream_t stream)
 {
     if (P.width > HELD) return tad_launch(tad_norm_forward_long_kernel<T>, (unsigned)std::min<int64_t>(P.n_rows, 2 * SMS), LARGE, 0, stream, P);
     const int threads = s.by == BY_WARP ? FORWARD_BLOCK : s.group, groups = s.by == BY_WARP ? FORWARD_BLOCK / 32 : 1;
     int64_t most = (int64_t)SMS * std::min(32, (eights ? FORWARD_BLOCKS : 2) * FORWARD_BLOCK / threads);
+    // Many fp32 rows: memory bounds them, and the SMs get unequal shares of it (8192 x 4096: the first blocks end at 31 us, the last at 46).  Five
+    // times the blocks, each with a fifth of the rows and at least three, even that out: 43 us for 48, 32768 x 4096 168 for 193.  16-bit rows
+    // are bound by instructions, there the blocks' starts cost more (26.6 -> 31.9), as they do with less to read than L2 holds.
+    if (sizeof(T) == 4 && eights && !keep && s.by == BY_GROUP && P.n_rows * P.width * 4 >= EVEN_BYTES && P.n_rows >= 16 * most) most *= EVEN;
     auto kernel = tad_norm_forward_kernel<T, 1, BY_WARP>;
     if (eights) kernel = s.by == BY_WARP ? tad_norm_forward_kernel<T, 8, BY_WARP> : s.by == BY_GROUP ? tad_norm_forward_kernel<T, 8, BY_GROUP> : tad_norm_forward_kernel<T, 8, BY_CLUSTER>;
     else if (s.by != BY_WARP) kernel = s.by == BY_GROUP ? tad_norm_forward_kernel<T, 1, BY_GROUP> : tad_norm_forward_kernel<T, 1, BY_CLUSTER>;
