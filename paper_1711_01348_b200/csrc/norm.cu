@@ -4,15 +4,15 @@
 //     g = dy w,  dx = rstd (g - sum g / D - xh sum (g xh) / D),  dw = sum_rows dy xh,  db = sum_rows dy
 //
 // Both passes read every element once and are bound by memory.  A row is held in registers, sixteen elements a thread, by a group of
-// 1 to 16 warps or, in longer rows, by a cluster of such groups; a group walks over the rows that are its share.  Rows of
+// 1 to 16 warps (of the forward pass, 32) or, in longer rows, by a cluster of such groups; a group walks over the rows that are its share.  Rows of
 // whole 16-byte pieces come by bulk copies into a ring of shared memory, two to four rows ahead (32 KB of rows under way a block of the
 // forward pass, 128 KB of the backward pass): prefetched into registers instead they take those that a second and third block
 // an SM need (8192 x 4096 fp32, forward / backward: 51 / 83 us for 48 / 69).  Other rows are loaded an element at a time, one row ahead.  The
 // variance is the mean of the squared deviations of the registers (no difference of large sums).  Weights stay in registers
 // over all rows.  The backward pass keeps its share of dw and db there too and writes them once a block, as a plane of partial
 // sums; a second kernel adds the planes up in a fixed order.  Rows longer than a cluster holds are read twice or three times.
-// Measured, 8192 x 4096: fp32 forward 48 us, backward 69 (5.6, 5.8 TB/s); bf16 27, 44 (5.0, 4.6 TB/s: converting an element and its
-// seven to ten operations take more than half of the issue slots, with the registers of 24 and 16 warps an SM).
+// Measured, 8192 x 4096: fp32 forward 43 us, backward 67 (6.2, 6.0 TB/s); bf16 26.5, 40 (5.1, 5.0 TB/s: of the backward pass the rows take 32, which
+// is the memory's rate, its start 2, the join of the partial sums in a block and of the blocks 1 and 2.7).
 #include <cooperative_groups.h>
 
 #include <atomic>
@@ -31,6 +31,9 @@ namespace cg = cooperative_groups;
 // spill, and what is spilled is waited for at once: 5003 x 1001 fp32 22 us for 17).
 constexpr int FORWARD_BLOCK = 256, FORWARD_BLOCKS = 3, BACKWARD_BLOCK = 512, FORWARD_E = 16;
 template <int V> constexpr int BACKWARD_E = V == 8 ? 16 : 8;
+// Rows that a block of 1024 threads holds: sixteen elements a thread, of 16-bit types thirty-two (four rows of 8192 at a time, not two).
+constexpr int WIDE_BLOCK = 1024;
+template <class T> constexpr int WIDE_E = sizeof(T) == 2 ? 32 : 16;
 constexpr int MAX_CLUSTER = 8;
 constexpr int HELD = FORWARD_BLOCK * FORWARD_E * MAX_CLUSTER;      // longest row that a cluster holds
 constexpr int LARGE = 1024, SMALL = 256;   // threads of a block of the kernels for longer rows
@@ -179,9 +182,9 @@ __device__ __forceinline__ bool wait_for(unsigned bar, unsigned parity)
 // Sums of N values over the threads of a group, the same bits in each of them.  A warp's sum goes into a box of shared
 // memory, everybody adds the boxes up in order; two sets of boxes are used in turn, so one barrier a sum is enough.  ALONE: the group
 // is the block.
-template <int N, int BY, bool ALONE>
+template <int N, int BY, bool ALONE, int WARPS>
 struct Sum {
-    float (*box)[BACKWARD_BLOCK / 32][N];  // [2], of this block
+    float (*box)[WARPS][N];                // [2], of this block
     int first, warps, id, threads;         // this group: its first warp, its warps, its barrier and its threads
     int turn;
     __device__ __forceinline__ void of(float (&v)[N])
@@ -203,7 +206,7 @@ struct Sum {
         else asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
         float2 both = make_float2(0.f, 0.f);                       // N = 2: the two sums; N = 1: of the even and of the odd warps
 #pragma unroll
-        for (int w = 0; w < BACKWARD_BLOCK / 32; w += 2) {         // (groups have an even number of warps)
+        for (int w = 0; w < WARPS; w += 2) {                       // (groups have an even number of warps)
             if (w >= warps) break;
             if (N == 2) {
                 const float4 p = *reinterpret_cast<const float4 *>(&box[turn][first + w][0]);
@@ -287,11 +290,11 @@ struct Place {
     }
 };
 
-template <int N, int BY, bool ALONE>
-__device__ __forceinline__ Sum<N, BY, ALONE> sum_of(const Params &P, float (*box)[BACKWARD_BLOCK / 32][N])
+template <int N, int BY, bool ALONE, int WARPS>
+__device__ __forceinline__ Sum<N, BY, ALONE, WARPS> sum_of(const Params &P, float (*box)[WARPS][N])
 {
     const int g = BY == BY_CLUSTER ? 0 : threadIdx.x / P.group;
-    return Sum<N, BY, ALONE>{box, g * (P.group >> 5), P.group >> 5, 1 + g, P.group, 0};
+    return Sum<N, BY, ALONE, WARPS>{box, g * (P.group >> 5), P.group >> 5, 1 + g, P.group, 0};
 }
 
 // ---- rows ahead ----
@@ -393,18 +396,21 @@ __device__ __forceinline__ void keep_row(const Params &P, int64_t r, int col, in
     }
 }
 
-// V = 8: width and all row starts are whole pieces of eight.  KEEP: with the checkpoint of fp32 rows.
-template <class T, int V, int BY, bool KEEP = false>
-__global__ void __launch_bounds__(FORWARD_BLOCK, V == 1 ? 2 : FORWARD_BLOCKS)
+// V = 8: width and all row starts are whole pieces of eight.  KEEP: with the checkpoint of fp32 rows.  WIDE: rows beyond what a block of 256 holds, by
+// groups of a block of up to 1024 threads with so many stages; the weights lie in shared memory, where they take no registers.  (By clusters, with an
+// exchange a row, bf16: 8192 x 5120 80 us for 32.5, 8192 x 6144 80 for 34, 4096 x 8192 43 for 26, 2048 x 16384 50 for 35.  Two rows of a group at a
+// time, whose sums share barriers, with sixteen elements of each a thread: 43, 56, 38.)
+template <class T, int V, int BY, bool KEEP = false, int WIDE = 0>
+__global__ void __launch_bounds__(WIDE ? WIDE_BLOCK : FORWARD_BLOCK, WIDE ? 1 : V == 1 ? 2 : FORWARD_BLOCKS)
 tad_norm_forward_kernel(const Params P)
 {
-    constexpr int E = FORWARD_E, STAGES = FORWARD_STAGES<T>;
-    __shared__ __align__(16) float box[2][BACKWARD_BLOCK / 32][1];
+    constexpr int E = WIDE ? WIDE_E<T> : FORWARD_E, STAGES = WIDE ? WIDE : FORWARD_STAGES<T>, WARPS = (WIDE ? WIDE_BLOCK : FORWARD_BLOCK) / 32;
+    __shared__ __align__(16) float box[2][WARPS][1];
     __shared__ Exchange ex;
-    __shared__ unsigned long long bars[FORWARD_BLOCK / 32][STAGES];
+    __shared__ unsigned long long bars[WARPS][STAGES];
     extern __shared__ __align__(128) unsigned char rows[];
     tad_wait_previous();
-    Sum<1, BY, true> sum = sum_of<1, BY, true>(P, box);
+    Sum<1, BY, !WIDE, WARPS> sum = sum_of<1, BY, !WIDE, WARPS>(P, box);
     const Place<BY, V, E> at(P);
     int64_t r = at.row;
     const T *__restrict__ x = static_cast<const T *>(P.x);
@@ -426,8 +432,22 @@ tad_norm_forward_kernel(const Params P)
         next.zero();
         if (r < P.n_rows) next.fetch(x + r * P.xs + at.col, at.rem);
     }
-    Pairs<E> w, b;
-    {
+    Pairs<WIDE ? 2 : E> w, b;
+    // WIDE: four planes of float4, weights and biases 0 .. 3 and 4 .. 7 of every eight columns
+    const unsigned eights = P.group * E / 8;
+    float4 *const vectors = reinterpret_cast<float4 *>(rows + (size_t)blockDim.x * E * STAGES * sizeof(T));
+    if constexpr (WIDE) {
+        for (unsigned c = threadIdx.x; c < eights; c += blockDim.x) {
+            float f[8], g[8];
+            load_vector<8, 8>(f, P.w, P.w_type, c * 8, P.width - (int)c * 8, 1.f);
+            load_vector<8, 8>(g, P.b, P.b_type, c * 8, P.width - (int)c * 8, 0.f);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                vectors[h * eights + c] = make_float4(f[4 * h], f[4 * h + 1], f[4 * h + 2], f[4 * h + 3]);
+                vectors[(2 + h) * eights + c] = make_float4(g[4 * h], g[4 * h + 1], g[4 * h + 2], g[4 * h + 3]);
+            }
+        }
+    } else {
         float f[E];
         load_vector<V, E>(f, P.w, P.w_type, at.col, at.rem, 1.f);
         w.set(f);
@@ -501,7 +521,13 @@ tad_norm_forward_kernel(const Params P)
         }
         const float2 rr = make_float2(rstd, rstd);
 #pragma unroll
-        for (int j = 0; j < E / 2; ++j) u.p[j] = __ffma2_rn(__fmul2_rn(u.p[j], rr), w.p[j], b.p[j]);
+        for (int j = 0; j < E / 2; ++j) {
+            if constexpr (WIDE) {
+                const unsigned place = (j >> 1 & 1) * eights + at.col / 8 + Of<8>::place(j / 4) / 8;
+                const float4 ww = vectors[place], bb = vectors[2 * eights + place];
+                u.p[j] = __ffma2_rn(__fmul2_rn(u.p[j], rr), j & 1 ? make_float2(ww.z, ww.w) : make_float2(ww.x, ww.y), j & 1 ? make_float2(bb.z, bb.w) : make_float2(bb.x, bb.y));
+            } else u.p[j] = __ffma2_rn(__fmul2_rn(u.p[j], rr), w.p[j], b.p[j]);
+        }
         u.get(v);
         store_typed<V, E>(P.y, P.y_type, r * P.ys + at.col, at.rem, v);
     }
@@ -662,7 +688,7 @@ tad_norm_backward_kernel(const Params P)
     extern __shared__ __align__(128) unsigned char rows[];
     __shared__ __align__(16) float join[V == 8 || BY == BY_CLUSTER ? 1 : 2 * E * BACKWARD_BLOCK];
     tad_wait_previous();
-    Sum<2, BY, BY == BY_CLUSTER> sum = sum_of<2, BY, BY == BY_CLUSTER>(P, box);
+    Sum<2, BY, BY == BY_CLUSTER, BACKWARD_BLOCK / 32> sum = sum_of<2, BY, BY == BY_CLUSTER, BACKWARD_BLOCK / 32>(P, box);
     const Place<BY, V, E> at(P);
     int64_t r = at.row;
     const T *__restrict__ dy = static_cast<const T *>(P.dy);
@@ -964,6 +990,19 @@ cudaError_t clusters_of(K kernel, int threads, size_t smem, int cluster, std::at
     return cudaSuccess;
 }
 
+// dynamic shared memory of a kernel beyond 48 KB, once a device
+template <class K>
+cudaError_t allow(K kernel, size_t most, std::atomic<bool> (&known)[64])
+{
+    int dev = -1;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess || (dev >= 0 && dev < 64 && known[dev].load(std::memory_order_relaxed))) return e;
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most);
+    if (e == cudaSuccess && dev >= 0 && dev < 64) known[dev].store(true, std::memory_order_relaxed);
+    return e;
+}
+
+constexpr size_t WIDE_ROOM = 220 * 1024;
 constexpr int64_t EVEN_BYTES = 96000000;
 constexpr int EVEN = 5;
 
@@ -971,6 +1010,26 @@ template <class T>
 cudaError_t forward(const Params &P, const Shape &s, bool eights, bool keep, cudaStream_t stream)
 {
     if (P.width > HELD) return tad_launch(tad_norm_forward_long_kernel<T>, (unsigned)std::min<int64_t>(P.n_rows, 2 * SMS), LARGE, 0, stream, P);
+    // Rows that a cluster would hold, by one block.  (Of few rows a cluster each is faster: 16 x 16384 4.5 us for 6.6, 200 x 8192 5.4 for 6.4, 300 x 8192
+    // 6.9 for 6.7, 1000 x 8192 14 for 10.  Rows up to 4096 in this form: 8192 x 4096 25.3 for 26.5, but 8192 x 2560 22.4 for 20.2, 20000 x 1024 25.6
+    // for 17.6, 1000 x 2048 5.6 for 4.5.)
+    if (eights && !keep && s.by == BY_CLUSTER && P.width <= WIDE_BLOCK * WIDE_E<T> && P.n_rows >= 2 * SMS) {
+        Params W = P;
+        W.group = (P.width + 64 * WIDE_E<T> - 1) / (64 * WIDE_E<T>) * 64;
+        const size_t held = (size_t)W.group * WIDE_E<T>, vectors = held * 8;
+        int groups = std::min(15, WIDE_BLOCK / W.group);           // (named barriers: one a group beside the block's)
+        while (groups > 1 && 2 * groups * held * sizeof(T) + vectors > WIDE_ROOM) --groups;
+        const int threads = groups * W.group;
+        const size_t stage = groups * held * sizeof(T);
+        static std::atomic<bool> allowed[2][64];
+        if (2 * stage + vectors <= WIDE_ROOM) {
+            const bool four = 4 * stage + vectors <= WIDE_ROOM;
+            auto kernel = four ? tad_norm_forward_kernel<T, 8, BY_GROUP, false, 4> : tad_norm_forward_kernel<T, 8, BY_GROUP, false, 2>;
+            const cudaError_t e = allow(kernel, WIDE_ROOM, allowed[four]);
+            if (e != cudaSuccess) return e;
+            return tad_launch(kernel, (unsigned)std::min<int64_t>((P.n_rows + groups - 1) / groups, SMS), threads, (four ? 4 : 2) * stage + vectors, stream, W);
+        }
+    }
     const int threads = s.by == BY_WARP ? FORWARD_BLOCK : s.group, groups = s.by == BY_WARP ? FORWARD_BLOCK / 32 : 1;
     int64_t most = (int64_t)SMS * std::min(32, (eights ? FORWARD_BLOCKS : 2) * FORWARD_BLOCK / threads);
     // Many fp32 rows: memory bounds them, and the SMs get unequal shares of it (8192 x 4096: the first blocks end at 31 us, the last at 46).  Five
@@ -1015,15 +1074,9 @@ cudaError_t backward(Params &P, bool eights, int64_t &planes, cudaStream_t strea
     if (eights) {
         constexpr size_t most = (size_t)BACKWARD_BLOCK * BACKWARD_E<8> * (SOURCE_BYTES<S> + sizeof(T)) * BACKWARD_STAGES<S, T>;
         static_assert(most <= 163840, "rows ahead and the join of the groups fit into shared memory");
-        static std::atomic<bool> allowed[64][3];
-        int dev = -1;
-        cudaError_t e = cudaGetDevice(&dev);
+        static std::atomic<bool> allowed[3][64];
+        const cudaError_t e = allow(kernel, most, allowed[s.by]);
         if (e != cudaSuccess) return e;
-        if (dev < 0 || dev >= 64 || !allowed[dev][s.by].load(std::memory_order_relaxed)) {
-            e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most);
-            if (e != cudaSuccess) return e;
-            if (dev >= 0 && dev < 64) allowed[dev][s.by].store(true, std::memory_order_relaxed);
-        }
         smem = (size_t)threads * BACKWARD_E<8> * (SOURCE_BYTES<S> + sizeof(T)) * BACKWARD_STAGES<S, T>;
     }
     if (s.cluster > 1) {

@@ -117,6 +117,50 @@ def test_rows(n, width):
     _run(n, width, "bf16", wkind="f32")
 
 
+@pytest.mark.parametrize("n,width", [(297, 4104), (703, 5000), (450, 6144), (299, 8192), (1000, 8200), (300, 12288), (301, 16376), (600, 16384)])
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+def test_many_wide_rows(n, width, kind):
+    _run(n, width, kind, wkind=kind, pad=8 * (n % 2), offset=16)
+
+
+def test_many_wide_rows_of_other_types():
+    _run(333, 8192, "bf16", ykind="f32", wkind="f32")
+    _run(333, 6144, "f32", ykind="bf16", wkind="f16")
+    _run(333, 5008, "bf16", affine=False)
+    _run(333, 4800, "f32", packed=True)
+
+
+def test_many_wide_rows_without_statistics_and_with_weights_off_every_boundary():
+    n, width = 500, 7176
+    x, _, w, b = _case(n, width, "bf16", 5)
+    X, Y, W, B = Matrix(n, width, "bf16", values=x), Matrix(n, width, "bf16"), Matrix(1, width, "bf16", offset=1, values=w), Matrix(1, width, "bf16", offset=3, values=b)
+    layernorm_forward(X.rows, n, width, Y.rows, W.rows, B.rows, 1e-5, stream=stream())
+    got = Y.double()
+    Y.check_guards()
+    mean, rstd = torch.empty(n, device="cuda"), torch.empty(n, device="cuda")
+    layernorm_forward(X.rows, n, width, Y.rows, W.rows, B.rows, 1e-5, mean.data_ptr(), rstd.data_ptr(), stream=stream())
+    assert torch.equal(got, Y.double())
+    _check_forward(X.double(), W.double(), B.double(), 1e-5, got, mean.double().cpu(), rstd.double().cpu(), "bf16")
+
+
+def test_many_wide_rows_with_infinities_stay_alone():
+    n, width = 400, 8192
+    x, _, w, b = _case(n, width, "bf16", 6)
+    X, Y, W, B = Matrix(n, width, "bf16", values=x), Matrix(n, width, "bf16"), Matrix(1, width, "f32", values=w), Matrix(1, width, "f32", values=b)
+    layernorm_forward(X.rows, n, width, Y.rows, W.rows, B.rows, 1e-5, stream=stream())
+    want = Y.double()
+    bad = torch.tensor([0, 7, 148, 399])
+    X.t[bad.cuda(), torch.tensor([0, 8191, 4000, 1023]).cuda()] = torch.tensor([float("inf"), float("nan"), float("-inf"), float("nan")], dtype=torch.bfloat16, device="cuda")
+    layernorm_forward(X.rows, n, width, Y.rows, W.rows, B.rows, 1e-5, stream=stream())
+    got, rest = Y.double(), torch.ones(n, dtype=torch.bool)
+    rest[bad] = False
+    assert torch.equal(got[rest], want[rest]) and bool(torch.isnan(got[bad]).all())
+
+
+def test_more_fp32_rows_than_the_second_level_cache_holds():
+    _run(9501, 2536, "f32")
+
+
 @pytest.mark.parametrize("kind,ykind,wkind", [("f32", "bf16", "f32"), ("bf16", "f32", "bf16"), ("f16", "bf16", "f16"), ("f32", "f16", "bf16")])
 @pytest.mark.parametrize("width,pad,offset", [(1024, 0, 0), (1024, 8, 8), (1024, 3, 1), (401, 5, 3), (8200, 0, 0)])
 def test_types_strides_offsets(kind, ykind, wkind, width, pad, offset):
