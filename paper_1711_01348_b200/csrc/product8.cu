@@ -437,6 +437,10 @@ struct Few {
     int type, many, few, k;
 };
 
+// A lane's sixteen elements lie in one block on either side.  Their products are summed as the codes stand for them (448^2 16 at most) and the
+// scales applied to the sum, as two powers of two of the same size: 2^120 times an element is beyond fp32, and so is its product with an element
+// of the other side, where that side's scale brings it back.  (The first factor loses digits of a sum only where the second
+// makes it less than the smallest fp32 number; where it gives an infinity, so does the second.)
 template <int F>
 __global__ void __launch_bounds__(128)
 tad_product8_few_kernel(const Few P)
@@ -455,27 +459,28 @@ tad_product8_few_kernel(const Few P)
         // (rows are a multiple of 16 bytes: the load is inside; what lies behind k counts as zero)
         const int left = P.k - k;
         uint4 w[FEW_ROWS];
-        float ws[FEW_ROWS];
+        unsigned ws[FEW_ROWS], xs[F];
 #pragma unroll
         for (int i = 0; i < FEW_ROWS; ++i) {
             const int64_t r = min(r0 + i, (int64_t)P.many - 1);
             w[i] = *reinterpret_cast<const uint4 *>(P.q + r * P.qs + k);
-            ws[i] = scale_of(P.s[r * P.ss + k / TAD_BLOCK8]);
+            ws[i] = (unsigned)P.s[r * P.ss + k / TAD_BLOCK8] << 23;
         }
         float x[F][16];
 #pragma unroll
         for (int f = 0; f < F; ++f) {
             const int g = min(f, P.few - 1);
             const uint4 u = *reinterpret_cast<const uint4 *>(P.fq + g * P.fqs + k);
-            const float s = scale_of(P.fs[g * P.fss + k / TAD_BLOCK8]);
+            xs[f] = (unsigned)P.fs[g * P.fss + k / TAD_BLOCK8] << 23;
             float lo[8], hi[8];
-            unpack_eight(make_uint2(u.x, u.y), s, lo);
-            unpack_eight(make_uint2(u.z, u.w), s, hi);
+            unpack_eight(make_uint2(u.x, u.y), 1.f, lo);
+            unpack_eight(make_uint2(u.z, u.w), 1.f, hi);
 #pragma unroll
             for (int j = 0; j < 8; ++j) { x[f][j] = lo[j]; x[f][8 + j] = hi[j]; }
             if (left < 16)
 #pragma unroll
                 for (int j = 0; j < 16; ++j) if (j >= left) x[f][j] = 0.f;
+            if (xs[f] == 255u << 23) x[f][0] = __uint_as_float(0x7fffffffu);           // (a block whose scale stands for NaN)
         }
 #pragma unroll
         for (int i = 0; i < FEW_ROWS; ++i) {
@@ -487,12 +492,15 @@ tad_product8_few_kernel(const Few P)
             if (left < 16)
 #pragma unroll
                 for (int j = 0; j < 16; ++j) if (j >= left) v[j] = 0.f;
+            if (ws[i] == 255u << 23) v[0] = __uint_as_float(0x7fffffffu);
 #pragma unroll
             for (int f = 0; f < F; ++f) {
                 float2 d = make_float2(0.f, 0.f);
 #pragma unroll
                 for (int j = 0; j < 16; j += 2) d = __ffma2_rn(make_float2(v[j], v[j + 1]), make_float2(x[f][j], x[f][j + 1]), d);
-                acc[i][f] = fmaf(d.x + d.y, ws[i], acc[i][f]);
+                // (the sum of two exponent bytes has nine bits; a byte of 0 is a factor 0 here instead of 2^-127, in results below 2^-230)
+                const unsigned both = ws[i] + xs[f], half = both >> 1 & 0x7f800000u;
+                acc[i][f] = fmaf((d.x + d.y) * __uint_as_float(half), __uint_as_float(both - half), acc[i][f]);
             }
         }
     }
