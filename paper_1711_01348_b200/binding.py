@@ -29,7 +29,7 @@ EXPORTS = ["tad_compile", "tad_destroy", "tad_workspace_bytes", "tad_forward", "
            "tad_plan_disassemble", "tad_plan_print", "tad_extended_euclid", "tad_smith_normal_form", "tad_fourier_motzkin",
            "tad_measure_fp32_rate",
            "tad_pack8", "tad_unpack8", "tad_repack8", "tad_layernorm_forward", "tad_layernorm_workspace_bytes",
-           "tad_layernorm_backward", "tad_embed_forward", "tad_embed_workspace_bytes", "tad_embed_backward",
+           "tad_layernorm_backward", "tad_debug_lost_waits", "tad_embed_forward", "tad_embed_workspace_bytes", "tad_embed_backward",
            "tad_matmul8_workspace_bytes", "tad_matmul8"]
 
 
@@ -142,6 +142,8 @@ def _load() -> C.CDLL:
     lib.tad_layernorm_forward.argtypes = [rows, i64, i64, rows, rows, flt, rows, vp, vp, packed, vp]
     lib.tad_layernorm_workspace_bytes.argtypes = [i64, i64]
     lib.tad_layernorm_backward.argtypes = [rows, rows, packed, i64, i64, rows, vp, vp, rows, rows, rows, vp, size, vp]
+    lib.tad_debug_lost_waits.argtypes = [i32]
+    lib.tad_debug_lost_waits.restype = None
     lib.tad_embed_forward.argtypes = [vp, i32, i64, rows, i64, i64, flt, rows, vp]
     lib.tad_embed_workspace_bytes.argtypes = [i64, i64, i64]
     lib.tad_embed_backward.argtypes = [vp, i32, i64, rows, i64, i64, flt, rows, i32, vp, size, vp]
@@ -355,6 +357,11 @@ def layernorm_backward(dy: Rows, x: Optional[Rows], checkpoint: Optional[Packed]
     """From x or from its checkpoint: one of the two is None."""
     _check(lib.tad_layernorm_backward(dy, x, checkpoint, n_rows, width, weight, mean_ptr or None, rstd_ptr or None, dx, dweight, dbias,
                                       workspace_ptr or None, workspace_bytes, stream or None))
+
+
+def debug_lost_waits(lost: bool) -> None:
+    """Waits in the layer norm's kernels count as run out from now on, or no longer (tests)."""
+    lib.tad_debug_lost_waits(int(lost))
 
 
 def embed_forward(tokens_ptr: int, token_bits: int, n_tokens: int, table: Rows, n_table: int, width: int, factor: float, y: Rows,

@@ -52,6 +52,7 @@ struct Params {
     int width, w_type, b_type, y_type, dx_type;
     int group;                             // threads of a group
     float eps, inv_width;
+    int lost;                              // waits count as run out (tests)
 };
 
 // How rows are divided: a warp a row, a group of warps, a cluster of groups (a block each).
@@ -164,6 +165,10 @@ __device__ __forceinline__ float warp_sum(float v)
     return v;
 }
 
+// A thread whose wait has run out is lost: it waits no more, and what the data were for is NaN from here on.  What is on its way into the block's
+// memory must not land there when the block, or the next one, uses that for something else: behind the loop over the rows a lost thread lingers
+// (about a millisecond; copies were issued before the wait that has run out began, values of other blocks take a microsecond).  Waiting
+// for each of them instead takes registers and time in the loop, 2 - 15 % of it.
 constexpr long long WAIT_LIMIT = 1ll << 31;        // clocks (about a second) after which a wait gives up
 __device__ __forceinline__ bool wait_once(unsigned bar, unsigned parity)
 {
@@ -177,6 +182,19 @@ __device__ __forceinline__ bool wait_for(unsigned bar, unsigned parity)
     const long long begin = clock64();
     while (clock64() - begin < WAIT_LIMIT) if (wait_once(bar, parity)) return true;
     return false;
+}
+
+__device__ __forceinline__ void linger()
+{
+    const long long begin = clock64();
+    while (clock64() - begin < (1ll << 21)) { }
+}
+// (hides from the compiler that a flag is not set where a wait has ended well: it would make two loops over the rows of it, 4 - 6 % slower in clusters)
+__device__ __forceinline__ void keep_one_loop(bool &flag)
+{
+    int f = flag;
+    asm volatile("" : "+r"(f));
+    flag = f;
 }
 
 // Sums of N values over the threads of a group, the same bits in each of them.  A warp's sum goes into a box of shared
@@ -229,10 +247,10 @@ struct Exchange {
 struct Trade {
     Exchange *ex;
     unsigned blocks, rank, count;
-    bool lost;                             // a wait has run out, there are no further ones
-    __device__ __forceinline__ void start(Exchange *e)
+    bool lost;                             // a lost thread sends nothing, a lost first thread arms no barrier: then nobody takes one row's values for another's
+    __device__ __forceinline__ void start(const Params &P, Exchange *e)
     {
-        ex = e; count = 0; lost = false;
+        ex = e; count = 0; lost = P.lost;
         cg::cluster_group cluster = cg::this_cluster();
         blocks = cluster.num_blocks();
         rank = cluster.block_rank();
@@ -244,23 +262,28 @@ struct Trade {
         cluster.sync();
     }
     // the values of all blocks, in order.  A barrier of the block lies between two trades: a block writes its values n + 2 behind everybody's
-    // values n + 1, which are sent behind that barrier and so behind the reads of the values n.
+    // values n + 1, which are sent behind that barrier and so behind the reads of the values n.  lost: they are not the values.
     __device__ __forceinline__ const float2 *with_all(float a, float b)
     {
         const unsigned turn = count & 1, parity = (count >> 1) & 1, bar = (unsigned)__cvta_generic_to_shared(&ex->bar[turn]);
         ++count;
-        if (threadIdx.x == 0) asm volatile("{ .reg .b64 t; mbarrier.arrive.expect_tx.shared::cta.b64 t, [%0], %1; }" ::"r"(bar), "r"(blocks * 8) : "memory");
-        if (threadIdx.x < blocks) {
+        if (threadIdx.x == 0 && !lost) asm volatile("{ .reg .b64 t; mbarrier.arrive.expect_tx.shared::cta.b64 t, [%0], %1; }" ::"r"(bar), "r"(blocks * 8) : "memory");
+        if (threadIdx.x < blocks && !lost) {
             unsigned to, at;
             asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"((unsigned)__cvta_generic_to_shared(&ex->far[turn][rank])), "r"(threadIdx.x));
             asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(bar), "r"(threadIdx.x));
             asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.b32 [%0], {%1, %2}, [%3];" ::"r"(to), "r"(__float_as_uint(a)), "r"(__float_as_uint(b)), "r"(at) : "memory");
         }
         if (!lost) lost = !wait_for(bar, parity);
+        keep_one_loop(lost);
         return ex->far[turn];
     }
-    // no block leaves while another one may still write into it
-    __device__ __forceinline__ void finish() { cg::this_cluster().sync(); }
+    // no block leaves while another one may still write into it; a lost one has not seen all values arrive (behind the barrier all are sent)
+    __device__ __forceinline__ void finish()
+    {
+        cg::this_cluster().sync();
+        if (lost) linger();
+    }
 };
 
 // this thread's place: its group in the grid, the groups of the grid, its first column
@@ -307,12 +330,12 @@ template <int STAGES>
 struct Ring {
     unsigned buf, bars, stage_bytes;       // this group's rows (offset in `rows`) and barriers
     unsigned char *rows;
-    bool leader, lost;                     // lost: a wait has run out, there are no further waits and copies
+    bool leader, lost;                     // a lost leader issues no further copies
     int at;                                // the stage of the next row
     unsigned parity;
-    __device__ __forceinline__ void start(unsigned char *smem, unsigned offset, unsigned bar, unsigned bytes, bool first)
+    __device__ __forceinline__ void start(unsigned char *smem, unsigned offset, unsigned bar, unsigned bytes, bool first, bool lost_before)
     {
-        rows = smem; buf = offset; bars = bar; stage_bytes = bytes; leader = first; lost = false; at = 0; parity = 0;
+        rows = smem; buf = offset; bars = bar; stage_bytes = bytes; leader = first; lost = lost_before; at = 0; parity = 0;
         if (leader) {
 #pragma unroll
             for (int i = 0; i < STAGES; ++i) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bars + 8 * i) : "memory");
@@ -336,11 +359,10 @@ struct Ring {
 #pragma unroll
             for (int i = 0; i < STAGES; ++i) *reinterpret_cast<uint4 *>(rows + buf + i * stage_bytes + b) = make_uint4(0, 0, 0, 0);
     }
-    // waits for the row at the ring's head (a second at most)
-    __device__ __forceinline__ bool wait()
+    // waits for the row at the ring's head
+    __device__ __forceinline__ void wait()
     {
         if (!lost) lost = !wait_for(bars + 8 * at, parity);
-        return !lost;
     }
     __device__ __forceinline__ const unsigned char *row() const { return rows + buf + at * stage_bytes; }
     __device__ __forceinline__ void advance() { if (++at == STAGES) { at = 0; parity ^= 1; } }
@@ -369,8 +391,8 @@ __device__ __forceinline__ void elements(float (&v)[E], const Piece<T, 8> (&p)[E
 
 template <class T> constexpr int FORWARD_STAGES = sizeof(T) == 2 ? 4 : 2;
 
-// fp32 into 8 bits beside the pass: sixteen neighbouring threads hold a block of 128
-__device__ __forceinline__ void keep_row(const Params &P, int64_t r, int col, int rem, const float (&v)[FORWARD_E])
+// fp32 into 8 bits beside the pass: sixteen neighbouring threads hold a block of 128.  lost: NaNs
+__device__ __forceinline__ void keep_row(const Params &P, int64_t r, int col, int rem, const float (&v)[FORWARD_E], bool lost)
 {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -390,8 +412,9 @@ __device__ __forceinline__ void keep_row(const Params &P, int64_t r, int col, in
         const float inv = inverse_scale(byte);
         if (Of<8>::place(i) >= rem) continue;
         const int c = col + Of<8>::place(i);
-        *reinterpret_cast<uint2 *>(P.kq + r * P.kqs + c) =
-            make_uint2(to_e4m3x2(f[0] * inv, f[1] * inv) | (to_e4m3x2(f[2] * inv, f[3] * inv) << 16), to_e4m3x2(f[4] * inv, f[5] * inv) | (to_e4m3x2(f[6] * inv, f[7] * inv) << 16));
+        uint2 u = make_uint2(to_e4m3x2(f[0] * inv, f[1] * inv) | (to_e4m3x2(f[2] * inv, f[3] * inv) << 16), to_e4m3x2(f[4] * inv, f[5] * inv) | (to_e4m3x2(f[6] * inv, f[7] * inv) << 16));
+        if (lost) u = make_uint2(0x7f7f7f7fu, 0x7f7f7f7fu);
+        *reinterpret_cast<uint2 *>(P.kq + r * P.kqs + c) = u;
         if ((threadIdx.x & 15) == 0) P.kscale[r * P.kss + c / TAD_BLOCK8] = (uint8_t)byte;
     }
 }
@@ -420,7 +443,7 @@ tad_norm_forward_kernel(const Params P)
     // the first rows are under way before anything else is done
     if constexpr (V != 1) {
         const unsigned stage = P.group * E * (unsigned)sizeof(T);
-        ring.start(rows, at.group * STAGES * stage, smem_u32(&bars[at.group][0]), stage, at.in == 0);
+        ring.start(rows, at.group * STAGES * stage, smem_u32(&bars[at.group][0]), stage, at.in == 0, !WIDE && P.lost);      // (WIDE: a register too many)
         if (ring.leader)
             for (int i = 0; i < STAGES; ++i)
                 if (r + i * at.step < P.n_rows) {
@@ -455,7 +478,7 @@ tad_norm_forward_kernel(const Params P)
         b.set(f);
     }
     Trade trade;
-    if constexpr (BY == BY_CLUSTER) trade.start(&ex);
+    if constexpr (BY == BY_CLUSTER) trade.start(P, &ex);
     else if constexpr (V != 1) __syncthreads();
     for (; r < P.n_rows; r += at.step) {
         float v[E];
@@ -464,7 +487,10 @@ tad_norm_forward_kernel(const Params P)
             Piece<T, 8> p[E / 8];
             read_row<T, E>(p, reinterpret_cast<const T *>(ring.row()) + (at.col - at.col0));
             elements<T, E>(v, p);
-            if constexpr (KEEP) keep_row(P, r, at.col, at.rem, v);
+            if constexpr (KEEP) {
+                keep_one_loop(ring.lost);
+                keep_row(P, r, at.col, at.rem, v, ring.lost);
+            }
         } else {
             next.get(v);
             if (r + at.step < P.n_rows) next.fetch(x + (r + at.step) * P.xs + at.col, at.rem);
@@ -485,8 +511,7 @@ tad_norm_forward_kernel(const Params P)
             ring.advance();
         }
         // the mean, in a cluster that of the block's columns, and the squared deviations from it
-        const bool no_result = (V != 1 && ring.lost) || (BY == BY_CLUSTER && trade.lost);       // (a row or a block that never came)
-        const float total = no_result ? __uint_as_float(0x7fffffffu) : s[0];
+        const float total = V != 1 && ring.lost ? __uint_as_float(0x7fffffffu) : s[0];          // (a row that never came)
         float mean = BY == BY_CLUSTER ? (columns ? total / (float)columns : 0.f) : total * P.inv_width;
         two = make_float2(0.f, 0.f);
 #pragma unroll
@@ -500,7 +525,7 @@ tad_norm_forward_kernel(const Params P)
             // one exchange a row: the squares about the row's mean are those about a block's and the block's count times the squared distance
             // of the two
             const float2 *all = trade.with_all(total, s[0]);
-            float sums = 0.f, squares = 0.f;
+            float sums = trade.lost ? __uint_as_float(0x7fffffffu) : 0.f, squares = 0.f;            // (a block that never came)
             for (unsigned b = 0; b < trade.blocks; ++b) sums += all[b].x;
             const float whole = sums * P.inv_width;
             for (unsigned b = 0; b < trade.blocks; ++b) {
@@ -531,6 +556,8 @@ tad_norm_forward_kernel(const Params P)
         u.get(v);
         store_typed<V, E>(P.y, P.y_type, r * P.ys + at.col, at.rem, v);
     }
+    if constexpr (V != 1)
+        if (ring.lost) linger();
     if constexpr (BY == BY_CLUSTER) trade.finish();
 }
 
@@ -723,7 +750,7 @@ tad_norm_backward_kernel(const Params P)
     // the first rows are under way before anything else is done
     if constexpr (V == 8) {
         const unsigned stage = held * (SOURCE_BYTES<S> + (unsigned)sizeof(T));
-        ring.start(rows, at.group * STAGES * stage, smem_u32(&bars[at.group][0]), stage, at.in == 0);
+        ring.start(rows, at.group * STAGES * stage, smem_u32(&bars[at.group][0]), stage, at.in == 0, P.lost);
         if (ring.leader)
             for (int i = 0; i < STAGES; ++i) if (r + i * at.step < P.n_rows) issue(i, r + i * at.step);
         ring.zeros(x_bytes, held * SOURCE_BYTES<S>, at.in, P.group);
@@ -742,7 +769,7 @@ tad_norm_backward_kernel(const Params P)
         w.set(f);
     }
     Trade trade;
-    if constexpr (BY == BY_CLUSTER) trade.start(&ex);
+    if constexpr (BY == BY_CLUSTER) trade.start(P, &ex);
     else if constexpr (V == 8) __syncthreads();
 #pragma unroll
     for (int j = 0; j < E / 2; ++j) dws.p[j] = dbs.p[j] = make_float2(0.f, 0.f);
@@ -778,7 +805,7 @@ tad_norm_backward_kernel(const Params P)
             ndy.get(d);
         }
         fetch(r + at.step);
-        if (V == 8 && ring.lost) rstd = __uint_as_float(0x7fffffffu);        // (a row that never came has no result)
+        if (V == 8 && ring.lost) rstd = __uint_as_float(0x7fffffffu);        // (a row that never came has no result; dw and db: below)
         Pairs<E> h, dp;
         h.set(xh);
         dp.set(d);
@@ -818,8 +845,13 @@ tad_norm_backward_kernel(const Params P)
             store_typed<V, E>(P.dx, P.dx_type, r * P.dxs + at.col, at.rem, d);
         }
     }
+    if constexpr (V == 8)
+        if (ring.lost) linger();
     if constexpr (BY == BY_CLUSTER) trade.finish();
     if (!P.planes) return;
+    if (V == 8 && ring.lost)
+#pragma unroll
+        for (int j = 0; j < E / 2; ++j) dws.p[j] = dbs.p[j] = make_float2(__uint_as_float(0x7fffffffu), __uint_as_float(0x7fffffffu));
     float dw[E], db[E];
     dws.get(dw);
     dbs.get(db);
@@ -1002,6 +1034,8 @@ cudaError_t allow(K kernel, size_t most, std::atomic<bool> (&known)[64])
     return e;
 }
 
+std::atomic<int> lost_waits{0};            // of the launches from now on (tad_debug_lost_waits)
+
 constexpr size_t WIDE_ROOM = 220 * 1024;
 constexpr int64_t EVEN_BYTES = 96000000;
 constexpr int EVEN = 5;
@@ -1093,6 +1127,8 @@ cudaError_t backward(Params &P, bool eights, int64_t &planes, cudaStream_t strea
 
 extern "C" {
 
+void tad_debug_lost_waits(int32_t lost) { lost_waits.store(lost != 0, std::memory_order_relaxed); }
+
 tad_status tad_layernorm_forward(const tad_rows *x, int64_t n_rows, int64_t width, const tad_rows *weight, const tad_rows *bias,
                                  float eps, const tad_rows *y, float *mean, float *rstd, const tad_packed *checkpoint,
                                  void *cuda_stream)
@@ -1118,6 +1154,7 @@ tad_status tad_layernorm_forward(const tad_rows *x, int64_t n_rows, int64_t widt
     if (bias) { P.b = bias->data; P.b_type = bias->type; }
     P.mean = mean; P.rstd = rstd;
     P.n_rows = n_rows; P.width = (int)width; P.eps = eps; P.inv_width = 1.f / (float)width;
+    P.lost = lost_waits.load(std::memory_order_relaxed);
     const Shape s = shape_of(width, FORWARD_BLOCK, FORWARD_E);
     P.group = s.group;
     const bool eights = width % 8 == 0 && by_eights(x) && by_eights(y);
@@ -1170,6 +1207,7 @@ tad_status tad_layernorm_backward(const tad_rows *dy, const tad_rows *x, const t
         P.mean = const_cast<float *>(mean); P.rstd = const_cast<float *>(rstd);
         P.planes = sums ? static_cast<float *>(workspace) : nullptr;
         P.n_rows = n_rows; P.width = (int)width; P.inv_width = 1.f / (float)width;
+        P.lost = lost_waits.load(std::memory_order_relaxed);
         const bool eights = width % 8 == 0 && by_eights(dy) && (!x || by_eights(x)) && (!dx || by_eights(dx));
         TAD_WITH_TYPE(dy->type, T, {
             if (!x) e = backward<Packed8, T>(P, eights, planes, stream);
