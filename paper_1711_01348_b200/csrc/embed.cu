@@ -27,10 +27,12 @@ struct Tokens {
     const void *p;
     int bits;
     unsigned n_table;
-    __device__ __forceinline__ unsigned key(int64_t t) const
+    __device__ __forceinline__ unsigned inside(long long k) const { return k >= 0 && k < (long long)n_table ? (unsigned)k : n_table; }
+    __device__ __forceinline__ unsigned key(int64_t t) const { return inside(bits == 32 ? (long long)static_cast<const int *>(p)[t] : static_cast<const long long *>(p)[t]); }
+    // past the first-level cache
+    __device__ __forceinline__ unsigned key_from_l2(int64_t t) const
     {
-        const long long k = bits == 32 ? (long long)static_cast<const int *>(p)[t] : static_cast<const long long *>(p)[t];
-        return k >= 0 && k < (long long)n_table ? (unsigned)k : n_table;
+        return inside(bits == 32 ? (long long)__ldcg(static_cast<const int *>(p) + t) : __ldcg(static_cast<const long long *>(p) + t));
     }
 };
 
@@ -191,7 +193,8 @@ tad_embed_sort_kernel(const Tokens tok, const unsigned n, const unsigned run, co
 // Zeros into the rows that no token names, a share of consecutive rows a block.  The block reads all tokens for that: 4 bytes a token and
 // block out of L2, next to the share's rows themselves.  It runs beside the sort, which has waited for the kernels before both
 // by the time that this one starts (its blocks let it start behind their own wait), and waits for the sort at its end, so
-// that who waits for this kernel has waited for both.  (105000 rows of 2048 fp32 158 us, 5.4 TB/s.)
+// that who waits for this kernel has waited for both.  Its own wait is what would make earlier kernels' writes visible to its first-level caches,
+// so it reads the tokens from L2, where the sort's wait has them.  (105000 rows of 2048 fp32 158 us, 5.4 TB/s.)
 constexpr int CLEAR_NT = 1024;
 constexpr unsigned MAP_ROWS = 32768;                           // rows whose use is noted at a time, a bit each
 
@@ -210,7 +213,7 @@ tad_embed_clear_kernel(const Tokens tok, const unsigned n, const int64_t each, u
         __syncthreads();
 #pragma unroll 4
         for (int64_t t = threadIdx.x; t < n; t += CLEAR_NT) {
-            const int64_t at = (int64_t)tok.key(t) - r0;
+            const int64_t at = (int64_t)tok.key_from_l2(t) - r0;
             if (at >= 0 && at < rows) {
                 const unsigned bit = 1u << (at & 31);
                 if (!(*(volatile unsigned *)&map[at >> 5] & bit)) atomicOr(&map[at >> 5], bit);

@@ -1,8 +1,11 @@
 // Launches with programmatic stream serialisation: the next kernel of a stream becomes resident while the one before it
-// still runs and waits for it on the device.  Every kernel calls tad_wait_previous() before it touches global memory and
+// still runs and waits for it on the device.  Every kernel but one calls tad_wait_previous() before it touches global memory and
 // only then lets its own successor start, so at most two kernels of a stream are resident and no kernel reads or
-// writes anything before its predecessor has finished.  Steps of a dozen short kernels are bound by the gaps between
-// them: see the figures at each change of the launch count.
+// writes anything before its predecessor has finished.  The one is tad_embed_clear_kernel, which runs beside its predecessor, the
+// sort of the tokens: that has waited for all kernels before both when it lets this one start; the two share no memory that
+// either writes; and the clearing waits for the sort before it ends, so that its successor has waited for both.  It must
+// follow the sort directly.  Steps of a dozen short kernels are bound by the gaps between them: see the figures at each change of
+// the launch count.
 #pragma once
 #include <cuda_runtime.h>
 
