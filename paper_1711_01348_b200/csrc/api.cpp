@@ -9,7 +9,9 @@
 
 namespace tad {
 thread_local std::string g_last_error;
-void set_error(const std::string &m) { g_last_error = m; }
+// (no exception may leave the C entry points: without memory for it there is no text, the status says what there is to say)
+void set_error(const char *m) noexcept { try { g_last_error = m; } catch (...) { g_last_error.clear(); } }
+void set_error(const std::string &m) { set_error(m.c_str()); }
 
 template <class F> tad_status guarded(F &&f)
 {

@@ -500,10 +500,10 @@ Layout layout_of(int64_t n, int64_t width)
 
 tad_status check_tokens(const char *what, const void *tokens, int32_t bits, int64_t n, int64_t n_table)
 {
-    if (bits != 32 && bits != 64) return bad(std::string(what) + ": tokens have 32 or 64 bits");
-    if (n_table < 0) return bad(std::string(what) + ": negative size");
-    if (n_table >= MAX_ROWS) { tad::set_error(std::string(what) + ": 2^31 table rows and more"); return TAD_ERR_UNSUPPORTED; }
-    if (n > 0 && (!tokens || reinterpret_cast<uintptr_t>(tokens) % (bits / 8))) return bad(std::string(what) + ": tokens NULL or not aligned");
+    if (bits != 32 && bits != 64) return bad(what, "tokens have 32 or 64 bits");
+    if (n_table < 0) return bad(what, "negative size");
+    if (n_table >= MAX_ROWS) return refuse(TAD_ERR_UNSUPPORTED, what, "2^31 table rows and more");
+    if (n > 0 && (!tokens || reinterpret_cast<uintptr_t>(tokens) % (bits / 8))) return bad(what, "tokens NULL or not aligned");
     return TAD_OK;
 }
 
@@ -538,7 +538,7 @@ tad_status tad_embed_forward(const void *tokens, int32_t token_bits, int64_t n_t
         (st = check_rows("embed_forward: table", table, n_table, width)) || (st = check_rows("embed_forward: y", y, n_tokens, width))) return st;
     if (n_tokens == 0 || width == 0) return TAD_OK;
     // more blocks than a launch has, in either form (of matrices beyond any memory)
-    if (n_tokens * odd_chunks(width) >= MAX_ROWS * (NT / 32) - NT) { tad::set_error("embed_forward: too many blocks"); return TAD_ERR_UNSUPPORTED; }
+    if (n_tokens * odd_chunks(width) >= MAX_ROWS * (NT / 32) - NT) return refuse(TAD_ERR_UNSUPPORTED, "embed_forward", "too many blocks");
     const Tokens tok{tokens, token_bits, (unsigned)n_table};
     cudaError_t e = cudaSuccess;
     TAD_WITH_TYPE(table->type, S, TAD_WITH_TYPE(y->type, T, e = (embed_forward<S, T>(tok, n_tokens, table, width, factor, y, (cudaStream_t)cuda_stream))));

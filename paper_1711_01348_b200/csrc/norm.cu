@@ -1139,11 +1139,11 @@ tad_status tad_layernorm_forward(const tad_rows *x, int64_t n_rows, int64_t widt
     if (weight && (st = check_rows("layernorm_forward: weight", weight, 1, width, true))) return st;
     if (bias && (st = check_rows("layernorm_forward: bias", bias, 1, width, true))) return st;
     if (checkpoint && (st = check_packed("layernorm_forward: checkpoint", checkpoint, n_rows, width))) return st;
-    if (!(eps >= 0.f)) return bad("layernorm_forward: eps is negative or NaN");
-    if (reinterpret_cast<uintptr_t>(mean) % 4 || reinterpret_cast<uintptr_t>(rstd) % 4) return bad("layernorm_forward: mean or rstd not aligned");
+    if (!(eps >= 0.f)) return bad("layernorm_forward", "eps is negative or NaN");
+    if (reinterpret_cast<uintptr_t>(mean) % 4 || reinterpret_cast<uintptr_t>(rstd) % 4) return bad("layernorm_forward", "mean or rstd not aligned");
     if (n_rows == 0) return TAD_OK;
     if (width == 0) {
-        if (mean || rstd) return bad("layernorm_forward: rows of no elements have no mean");
+        if (mean || rstd) return bad("layernorm_forward", "rows of no elements have no mean");
         return TAD_OK;
     }
     const cudaStream_t stream = (cudaStream_t)cuda_stream;
@@ -1181,7 +1181,7 @@ tad_status tad_layernorm_backward(const tad_rows *dy, const tad_rows *x, const t
 {
     tad_status st;
     if ((st = check_sizes("layernorm_backward", n_rows, width)) || (st = check_rows("layernorm_backward: dy", dy, n_rows, width))) return st;
-    if (!x == !checkpoint) return bad("layernorm_backward: x or a checkpoint of it, one of the two");
+    if (!x == !checkpoint) return bad("layernorm_backward", "x or a checkpoint of it, one of the two");
     if (x && (st = check_rows("layernorm_backward: x", x, n_rows, width))) return st;
     if (checkpoint && (st = check_packed("layernorm_backward: checkpoint", checkpoint, n_rows, width))) return st;
     if (weight && (st = check_rows("layernorm_backward: weight", weight, 1, width, true))) return st;
@@ -1190,7 +1190,7 @@ tad_status tad_layernorm_backward(const tad_rows *dy, const tad_rows *x, const t
     if (dbias && (st = check_rows("layernorm_backward: dbias", dbias, 1, width, true))) return st;
     if (width == 0) return TAD_OK;
     if (n_rows > 0 && (!mean || !rstd || reinterpret_cast<uintptr_t>(mean) % 4 || reinterpret_cast<uintptr_t>(rstd) % 4))
-        return bad("layernorm_backward: mean or rstd NULL or not aligned");
+        return bad("layernorm_backward", "mean or rstd NULL or not aligned");
     const bool sums = dweight || dbias;
     if (sums && (st = check_room("layernorm_backward", workspace, workspace_bytes, tad_layernorm_workspace_bytes(n_rows, width)))) return st;
     if (!dx && !sums) return TAD_OK;

@@ -317,13 +317,13 @@ tad_status tad_launch_pack8(const tad_rows *x, int64_t n_rows, int64_t width, co
     cudaError_t e = cudaSuccess;
     if (by_eights(x)) {
         Launch l;
-        if (!cover(n_rows, tadr::blocks_of(width), OWN_PACK, l)) { tad::set_error("pack8: too many blocks"); return TAD_ERR_UNSUPPORTED; }
+        if (!cover(n_rows, tadr::blocks_of(width), OWN_PACK, l)) return refuse(TAD_ERR_UNSUPPORTED, "pack8", "too many blocks");
         TAD_WITH_TYPE(x->type, T,
             e = tad_launch(tad_pack8_kernel<T>, l.blocks, NT, 0, stream, static_cast<const T *>(x->data), x->stride, n_rows, (int)width, l.cb, l.chunks, out->q,
                            out->q_stride, out->scale, out->scale_stride));
     } else {
         unsigned blocks = 0, chunks = 0;
-        if (!odd_cover(n_rows, width, blocks, chunks)) { tad::set_error("pack8: too many blocks"); return TAD_ERR_UNSUPPORTED; }
+        if (!odd_cover(n_rows, width, blocks, chunks)) return refuse(TAD_ERR_UNSUPPORTED, "pack8", "too many blocks");
         TAD_WITH_TYPE(x->type, T,
             e = tad_launch(tad_pack8_odd_kernel<T>, blocks, NT, 0, stream, static_cast<const T *>(x->data), x->stride, n_rows, (int)width, chunks, out->q,
                            out->q_stride, out->scale, out->scale_stride));
@@ -350,13 +350,13 @@ tad_status tad_unpack8(const tad_packed *in, int64_t n_rows, int64_t width, cons
     cudaError_t e = cudaSuccess;
     if (by_eights(x)) {
         Launch l;
-        if (!cover(n_rows, blocks_of(width), OWN_UNPACK, l)) { tad::set_error("unpack8: too many blocks"); return TAD_ERR_UNSUPPORTED; }
+        if (!cover(n_rows, blocks_of(width), OWN_UNPACK, l)) return refuse(TAD_ERR_UNSUPPORTED, "unpack8", "too many blocks");
         TAD_WITH_TYPE(x->type, T,
             e = tad_launch(tad_unpack8_kernel<T>, l.blocks, NT, 0, stream, in->q, in->q_stride, in->scale, in->scale_stride, n_rows, (int)width, l.cb, l.chunks,
                            static_cast<T *>(x->data), x->stride));
     } else {
         unsigned blocks = 0, chunks = 0;
-        if (!odd_cover(n_rows, width, blocks, chunks)) { tad::set_error("unpack8: too many blocks"); return TAD_ERR_UNSUPPORTED; }
+        if (!odd_cover(n_rows, width, blocks, chunks)) return refuse(TAD_ERR_UNSUPPORTED, "unpack8", "too many blocks");
         TAD_WITH_TYPE(x->type, T,
             e = tad_launch(tad_unpack8_odd_kernel<T>, blocks, NT, 0, stream, in->q, in->q_stride, in->scale, in->scale_stride, n_rows, (int)width, chunks,
                            static_cast<T *>(x->data), x->stride));
@@ -372,7 +372,7 @@ tad_status tad_repack8(const tad_packed *in, int64_t n_rows, int64_t width, cons
     if (n_rows == 0 || width == 0) return TAD_OK;
     const unsigned tiles_c = (unsigned)blocks_of(width);
     const int64_t tiles = blocks_of(n_rows) * tiles_c;
-    if (tiles >= MAX_ROWS) { tad::set_error("repack8: too many tiles"); return TAD_ERR_UNSUPPORTED; }
+    if (tiles >= MAX_ROWS) return refuse(TAD_ERR_UNSUPPORTED, "repack8", "too many tiles");
     return launched("repack", tad_launch(tad_repack8_kernel, (unsigned)tiles, NT, 0, (cudaStream_t)cuda_stream, in->q, in->q_stride, in->scale,
                                          in->scale_stride, n_rows, (int)width, tiles_c, out->q, out->q_stride, out->scale, out->scale_stride));
 }

@@ -644,7 +644,7 @@ tad_status tad_matmul8(const tad_packed *a, const tad_packed *b, int64_t m, int6
     if (m == 0 || n == 0) return TAD_OK;
     const cudaStream_t stream = (cudaStream_t)cuda_stream;
     const int64_t elements = m * n;
-    if (elements >= (int64_t(1) << 38)) { tad::set_error("matmul8: 2^38 outputs and more"); return TAD_ERR_UNSUPPORTED; }
+    if (elements >= (int64_t(1) << 38)) return refuse(TAD_ERR_UNSUPPORTED, "matmul8", "2^38 outputs and more");
     if (k == 0) return launched("product", tad_launch(tad_product8_zero_kernel, (unsigned)((elements + 255) / 256), 256, 0, stream, m, (int)n, y->data, y->stride, (int)y->type));
     const Way w = way_of(m, n, k);
     if ((st = check_room("matmul8", workspace, workspace_bytes, tad_matmul8_workspace_bytes(m, n, k)))) return st;
@@ -668,7 +668,7 @@ tad_status tad_matmul8(const tad_packed *a, const tad_packed *b, int64_t m, int6
     P.blocks = w.blocks; P.each = w.each; P.split = w.split;
     P.tiles_p = (unsigned)w.tiles_p; P.tiles_q = (unsigned)w.tiles_q;
     const int64_t tiles = w.tiles_p * w.tiles_q * w.split;
-    if (tiles >= MAX_ROWS) { tad::set_error("matmul8: too many tiles"); return TAD_ERR_UNSUPPORTED; }
+    if (tiles >= MAX_ROWS) return refuse(TAD_ERR_UNSUPPORTED, "matmul8", "too many tiles");
     P.tiles = (unsigned)tiles;
     int64_t stride = y->stride;
     P.y = y->data; P.type = y->type;
@@ -676,7 +676,7 @@ tad_status tad_matmul8(const tad_packed *a, const tad_packed *b, int64_t m, int6
     P.yp = w.p_is_b ? 1 : stride; P.yq = w.p_is_b ? stride : 1;
     P.vec = !w.p_is_b && reinterpret_cast<uintptr_t>(P.y) % 32 == 0 && stride * (int64_t)type_size(P.type) % 32 == 0 && P.plane % 8 == 0;
     CUtensorMap mp, mq;
-    if (!map_of(&mp, p, P.np, k, BM) || !map_of(&mq, q, P.nq, k, w.pair ? w.bn / 2 : w.bn)) { tad::set_error("matmul8: no tensor map for this matrix (or no driver)"); return TAD_ERR_CUDA; }
+    if (!map_of(&mp, p, P.np, k, BM) || !map_of(&mq, q, P.nq, k, w.pair ? w.bn / 2 : w.bn)) return refuse(TAD_ERR_CUDA, "matmul8", "no tensor map for this matrix (or no driver)");
     e = w.pair ? launch_product<256, true>(mp, mq, P, stream) : w.bn == 256 ? launch_product<256, false>(mp, mq, P, stream) : w.bn == 128 ? launch_product<128, false>(mp, mq, P, stream) :
         w.bn == 64 ? launch_product<64, false>(mp, mq, P, stream) : launch_product<32, false>(mp, mq, P, stream);
     if (e == cudaSuccess && w.split > 1)

@@ -8,13 +8,13 @@
 
 #include <algorithm>
 #include <cstdint>
-#include <string>
+#include <cstdio>
 #include <type_traits>
 
 #include "../../include/tad.h"
 #include "launch.h"
 
-namespace tad { void set_error(const std::string &m); }
+namespace tad { void set_error(const char *m) noexcept; }
 
 namespace tadr {
 
@@ -23,12 +23,20 @@ constexpr int SMS = 148;                                  // of a B200: what gri
 
 // ---- host: checks ----
 
-inline tad_status bad(const std::string &m) { tad::set_error(m); return TAD_ERR_INVALID_ARG; }
+// (nothing here allocates: an exception may not leave the C entry points)
+inline tad_status refuse(tad_status status, const char *what, const char *why) noexcept
+{
+    char text[256];
+    std::snprintf(text, sizeof text, "%s: %s", what, why);
+    tad::set_error(text);
+    return status;
+}
+inline tad_status bad(const char *what, const char *why) noexcept { return refuse(TAD_ERR_INVALID_ARG, what, why); }
 
 inline tad_status check_sizes(const char *what, int64_t n_rows, int64_t width)
 {
-    if (n_rows < 0 || width < 0) return bad(std::string(what) + ": negative size");
-    if (n_rows >= MAX_ROWS || width >= MAX_WIDTH) { tad::set_error(std::string(what) + ": 2^31 rows or a width of 2^24 and more"); return TAD_ERR_UNSUPPORTED; }
+    if (n_rows < 0 || width < 0) return bad(what, "negative size");
+    if (n_rows >= MAX_ROWS || width >= MAX_WIDTH) return refuse(TAD_ERR_UNSUPPORTED, what, "2^31 rows or a width of 2^24 and more");
     return TAD_OK;
 }
 
@@ -37,13 +45,13 @@ inline size_t type_size(int type) { return type == TAD_F32 ? 4 : 2; }
 // vector: one row, the stride is not looked at
 inline tad_status check_rows(const char *what, const tad_rows *m, int64_t n_rows, int64_t width, bool vector = false)
 {
-    if (!m) return bad(std::string(what) + ": NULL matrix");
-    if (m->type != TAD_F32 && m->type != TAD_BF16 && m->type != TAD_F16) return bad(std::string(what) + ": unknown element type");
-    if (m->reserved != 0) return bad(std::string(what) + ": reserved field is not zero");
-    if (!vector && m->stride < width) return bad(std::string(what) + ": stride below the width");
+    if (!m) return bad(what, "NULL matrix");
+    if (m->type != TAD_F32 && m->type != TAD_BF16 && m->type != TAD_F16) return bad(what, "unknown element type");
+    if (m->reserved != 0) return bad(what, "reserved field is not zero");
+    if (!vector && m->stride < width) return bad(what, "stride below the width");
     if (n_rows == 0 || width == 0) return TAD_OK;
-    if (!m->data) return bad(std::string(what) + ": NULL data");
-    if (reinterpret_cast<uintptr_t>(m->data) % type_size(m->type)) return bad(std::string(what) + ": data not aligned to its element");
+    if (!m->data) return bad(what, "NULL data");
+    if (reinterpret_cast<uintptr_t>(m->data) % type_size(m->type)) return bad(what, "data not aligned to its element");
     return TAD_OK;
 }
 
@@ -51,29 +59,28 @@ inline int64_t blocks_of(int64_t width) { return (width + TAD_BLOCK8 - 1) / TAD_
 
 inline tad_status check_packed(const char *what, const tad_packed *m, int64_t n_rows, int64_t width)
 {
-    if (!m) return bad(std::string(what) + ": NULL packed matrix");
-    if (m->q_stride < width || m->scale_stride < blocks_of(width)) return bad(std::string(what) + ": stride below the width");
-    if (m->q_stride % 16 || m->scale_stride % 4) return bad(std::string(what) + ": q_stride must be a multiple of 16, scale_stride of 4");
+    if (!m) return bad(what, "NULL packed matrix");
+    if (m->q_stride < width || m->scale_stride < blocks_of(width)) return bad(what, "stride below the width");
+    if (m->q_stride % 16 || m->scale_stride % 4) return bad(what, "q_stride must be a multiple of 16, scale_stride of 4");
     if (n_rows == 0 || width == 0) return TAD_OK;
-    if (!m->q || !m->scale) return bad(std::string(what) + ": NULL data");
-    if (reinterpret_cast<uintptr_t>(m->q) % 16 || reinterpret_cast<uintptr_t>(m->scale) % 4) return bad(std::string(what) + ": q must be 16-byte aligned, scale 4-byte");
+    if (!m->q || !m->scale) return bad(what, "NULL data");
+    if (reinterpret_cast<uintptr_t>(m->q) % 16 || reinterpret_cast<uintptr_t>(m->scale) % 4) return bad(what, "q must be 16-byte aligned, scale 4-byte");
     return TAD_OK;
 }
 
 inline tad_status check_room(const char *what, const void *workspace, size_t bytes, size_t need)
 {
-    if (need && (!workspace || bytes < need || (reinterpret_cast<uintptr_t>(workspace) & 255u))) {
-        tad::set_error(std::string(what) + ": workspace missing, too small or not 256-byte aligned");
-        return TAD_ERR_WORKSPACE;
-    }
+    if (need && (!workspace || bytes < need || (reinterpret_cast<uintptr_t>(workspace) & 255u)))
+        return refuse(TAD_ERR_WORKSPACE, what, "workspace missing, too small or not 256-byte aligned");
     return TAD_OK;
 }
 
 inline tad_status launched(const char *what, cudaError_t e)
 {
     if (e == cudaSuccess) return TAD_OK;
-    tad::set_error(std::string(what) + " launch failed: " + cudaGetErrorString(e));
-    return TAD_ERR_CUDA;
+    char launch[64];
+    std::snprintf(launch, sizeof launch, "%s launch failed", what);
+    return refuse(TAD_ERR_CUDA, launch, cudaGetErrorString(e));
 }
 
 // rows that eight elements at a time can be read from and written to by one access of 16 or, fp32, 32 bytes
