@@ -343,10 +343,8 @@ tad_status tad_repack8(const tad_packed *in, int64_t n_rows, int64_t width, cons
  *                  gradients are those of the formula at the kept values, with the mean and rstd of the exact ones.
  *   dx, dweight, dbias   NULL = not wanted.  dx may have another type than x.  Without rows dweight and dbias are zeros.
  * Workspace: tad_layernorm_workspace_bytes, needed where dweight or dbias is wanted.
- * Waits inside the kernels (for a row's copy, for another block of a cluster) last about a second at most.  What a wait that ran out
- * was for is NaN: the rows of y and of the checkpoint, their mean and rstd, the rows of dx, all that they add to in dweight and dbias.
- * tad_debug_lost_waits(non-zero) makes them count as run out in launches of the process from then on, until it is called with zero: for
- * tests of what is left then.  (Not in the forward kernel for many rows of more than 4096 columns.)
+ * A wait inside the kernels (for a row's copy, for another block of a cluster) lasts about a second at most.  What a wait that ran out was
+ * for is NaN: the rows of y and of the checkpoint, their mean and rstd, the rows of dx, all that they add to in dweight and dbias.
  */
 tad_status tad_layernorm_forward(const tad_rows *x, int64_t n_rows, int64_t width, const tad_rows *weight, const tad_rows *bias,
                                  float eps, const tad_rows *y, float *mean, float *rstd, const tad_packed *checkpoint,
@@ -356,7 +354,6 @@ tad_status tad_layernorm_backward(const tad_rows *dy, const tad_rows *x, const t
                                   const tad_rows *weight, const float *mean, const float *rstd, const tad_rows *dx,
                                   const tad_rows *dweight, const tad_rows *dbias, void *workspace, size_t workspace_bytes,
                                   void *cuda_stream);
-void tad_debug_lost_waits(int32_t lost);
 
 /*
  * tad_embed_forward:  y[t] = factor * table[tokens[t]], a row of zeros where the token lies outside [0, n_table) (padding).
@@ -378,10 +375,18 @@ tad_status tad_embed_backward(const void *tokens, int32_t token_bits, int64_t n_
  * Forward, and both gradients, of a linear layer y = x w^T:  (x, w);  dx = (dy, w^T);  dw = (dy^T, x^T), the transposes by
  * tad_repack8.  NaN operands give NaN in the row or column they belong to.  m, n < 2^31, k < 2^24.
  * Workspace: tad_matmul8_workspace_bytes (may be 0); planes of partial sums of products with few outputs.
+ * A wait inside the kernel lasts about two seconds at most; the tiles that wanted what a wait that ran out was for are NaN.
  */
 size_t tad_matmul8_workspace_bytes(int64_t m, int64_t n, int64_t k);
 tad_status tad_matmul8(const tad_packed *a, const tad_packed *b, int64_t m, int64_t n, int64_t k, const tad_rows *y,
                        void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/*
+ * tad_debug_lost_waits(non-zero): waits in the kernels of the layer norm and of products on the tensor cores count as run out, in launches
+ * of the process from then on, until it is called with zero: for tests of what is left then.  (Not in the forward kernel of the layer
+ * norm for many rows of more than 4096 columns; of a product, a wait for a tile's operands.)
+ */
+void tad_debug_lost_waits(int32_t lost);
 
 /* ------------------------------------------------------------------------- */
 /* Introspection (host only).  These are what the bit-exact plan tests use.   */

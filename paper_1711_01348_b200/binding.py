@@ -359,11 +359,6 @@ def layernorm_backward(dy: Rows, x: Optional[Rows], checkpoint: Optional[Packed]
                                       workspace_ptr or None, workspace_bytes, stream or None))
 
 
-def debug_lost_waits(lost: bool) -> None:
-    """Waits in the layer norm's kernels count as run out from now on, or no longer (tests)."""
-    lib.tad_debug_lost_waits(int(lost))
-
-
 def embed_forward(tokens_ptr: int, token_bits: int, n_tokens: int, table: Rows, n_table: int, width: int, factor: float, y: Rows,
                   stream: int = 0) -> None:
     _check(lib.tad_embed_forward(tokens_ptr or None, token_bits, n_tokens, table, n_table, width, factor, y, stream or None))
@@ -386,6 +381,11 @@ def matmul8_workspace_bytes(m: int, n: int, k: int) -> int:
 def matmul8(a: Packed, b: Packed, m: int, n: int, k: int, y: Rows, workspace_ptr: int = 0, workspace_bytes: int = 0, stream: int = 0) -> None:
     """y = a b^T of packed matrices, a m x k and b n x k."""
     _check(lib.tad_matmul8(a, b, m, n, k, y, workspace_ptr or None, workspace_bytes, stream or None))
+
+
+def debug_lost_waits(lost: bool) -> None:
+    """Waits in the kernels of the layer norm and of products count as run out from now on, or no longer (tests)."""
+    lib.tad_debug_lost_waits(int(lost))
 
 
 # ---- host-only pieces of the integer algebra (for tests) ----

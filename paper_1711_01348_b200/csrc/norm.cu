@@ -21,6 +21,8 @@
 
 tad_status tad_launch_pack8(const tad_rows *x, int64_t n_rows, int64_t width, const tad_packed *out, cudaStream_t stream);
 
+std::atomic<int> tadr::lost_waits{0};
+
 namespace {
 
 using namespace tadr;
@@ -1033,8 +1035,6 @@ cudaError_t allow(K kernel, size_t most, std::atomic<bool> (&known)[64])
     if (e == cudaSuccess && dev >= 0 && dev < 64) known[dev].store(true, std::memory_order_relaxed);
     return e;
 }
-
-std::atomic<int> lost_waits{0};            // of the launches from now on (tad_debug_lost_waits)
 
 constexpr size_t WIDE_ROOM = 220 * 1024;
 constexpr int64_t EVEN_BYTES = 96000000;

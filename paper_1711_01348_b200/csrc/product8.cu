@@ -72,6 +72,12 @@ __device__ __forceinline__ void mbar_drain(unsigned bar, unsigned parity)
     const long long start = clock64();
     while (!__all_sync(0xffffffffu, mbar_try(bar, parity)) && !__any_sync(0xffffffffu, clock64() - start > WAIT_LIMIT)) { }
 }
+// about a millisecond: a thousand times what a copy takes
+__device__ __forceinline__ void linger()
+{
+    const long long start = clock64();
+    while (clock64() - start < (1ll << 21)) { }
+}
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tma_load(unsigned to, const CUtensorMap *map, int x, int y, unsigned bar)
@@ -133,6 +139,7 @@ struct Product {
     int type, vec;                                // vec: stores of 32 bytes along q
     int np, nq, blocks, each, split;              // sizes, blocks of k, blocks of a share of k, shares
     unsigned tiles_p, tiles_q, tiles;
+    int lost;                                     // a wait for a tile's operands counts as run out (tests)
 };
 
 template <int BN, bool PAIR> struct Config {
@@ -176,11 +183,11 @@ tad_product8_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_cons
     using C = Config<BN, PAIR>;
     constexpr int S = C::STAGES, TILE_P = PAIR ? 2 * BM : BM;
     extern __shared__ unsigned char smem_raw[];
-    __shared__ unsigned long long bars[2 * S + 2 * SF_BUFFERS + 2];
+    __shared__ unsigned long long bars[2 * S + 2 * SF_BUFFERS + 3];
     __shared__ unsigned tmem_base, spread[2][BM + (BN < 128 ? 128 : BN)];
     __shared__ volatile int failed;
     const unsigned smem0 = (smem_u32(smem_raw) + 1023u) & ~1023u;
-    const unsigned full = smem_u32(&bars[0]), empty = full + 8 * S, sf_full = empty + 8 * S, sf_empty = sf_full + 8 * SF_BUFFERS, acc_full = sf_empty + 8 * SF_BUFFERS, acc_empty = acc_full + 8;
+    const unsigned full = smem_u32(&bars[0]), empty = full + 8 * S, sf_full = empty + 8 * S, sf_empty = sf_full + 8 * SF_BUFFERS, acc_full = sf_empty + 8 * SF_BUFFERS, acc_empty = acc_full + 8, mma_end = acc_empty + 8;
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const unsigned rank = PAIR ? blockIdx.x & 1 : 0;                      // in the pair; the first block issues the MMAs
     const unsigned walker = PAIR ? blockIdx.x >> 1 : blockIdx.x, walkers = PAIR ? gridDim.x >> 1 : gridDim.x;
@@ -190,6 +197,7 @@ tad_product8_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_cons
             for (int i = 0; i < S; ++i) { mbar_init(full + 8 * i, 1); mbar_init(empty + 8 * i, 1); }
             for (int i = 0; i < SF_BUFFERS; ++i) { mbar_init(sf_full + 8 * i, PAIR ? 2 * SF_WARPS : SF_WARPS); mbar_init(sf_empty + 8 * i, 1); }
             mbar_init(acc_full, 1);
+            mbar_init(mma_end, 1);
             mbar_init(acc_empty, PAIR ? 2 * EPI_WARPS : EPI_WARPS);
             asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         }
@@ -242,7 +250,8 @@ tad_product8_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_cons
                 if (++at == S) at = 0;
             }
         }
-        // copies of a block that gave up still write its shared memory (of a pair: the first block knows)
+        // copies of a block that gave up still write its shared memory (of a pair: the first block's barriers know, of those that both have issued)
+        if (!ok && rank != 0) linger();
         if (!ok && rank == 0)
             for (unsigned long long i = issued > S ? issued - S : 0; i < issued; ++i) mbar_drain(full + 8 * (unsigned)(i % S), (unsigned)(i / S) & 1);
     } else if (warp == EPI_WARPS + SF_WARPS + 1) {
@@ -273,13 +282,16 @@ tad_product8_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_cons
                     if (++sf == SF_BUFFERS) { sf = 0; sf_phase ^= 1; }
                 }
             }
+            if (P.lost) { failed = 1; ok = false; }               // (not in the loop over k: 512 x 4096 x 4096 13.5 us for 11.9)
             if (ok) mma_commit<PAIR>(acc_full);
         }
-        // MMAs of a block that gave up still read its shared memory: all before this commit are done when it arrives (every other
-        // role has left or leaves its waits, and nothing else arrives at this barrier)
+        // MMAs of a block that gave up still read its shared memory: all are done when this commit arrives.  It has a barrier of its own, which
+        // nobody else waits at: at acc_full it would pass the part of a sum that there is for the sum.  (And copies that are under way behind
+        // those that were waited for get the time to land.)
         if (!ok && rank == 0) {
-            mma_commit<PAIR>(acc_full);
-            mbar_drain(acc_full, n & 1);
+            mma_commit<PAIR>(mma_end);
+            mbar_drain(mma_end, 0);
+            linger();
         }
     } else if (warp >= EPI_WARPS) {
         // ---- scales: lane l of every quarter of tensor memory holds rows l, 32 + l, ... in columns 0, 1, ..., the scale of one block a byte.
@@ -670,6 +682,7 @@ tad_status tad_matmul8(const tad_packed *a, const tad_packed *b, int64_t m, int6
     const int64_t tiles = w.tiles_p * w.tiles_q * w.split;
     if (tiles >= MAX_ROWS) return refuse(TAD_ERR_UNSUPPORTED, "matmul8", "too many tiles");
     P.tiles = (unsigned)tiles;
+    P.lost = lost_waits.load(std::memory_order_relaxed);
     int64_t stride = y->stride;
     P.y = y->data; P.type = y->type;
     if (w.split > 1) { P.y = workspace; P.type = TAD_F32; P.plane = elements; stride = n; }

@@ -7,6 +7,7 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <atomic>
 #include <cstdint>
 #include <cstdio>
 #include <type_traits>
@@ -15,6 +16,9 @@
 #include "launch.h"
 
 namespace tad { void set_error(const char *m) noexcept; }
+
+// waits in the kernels launched from now on count as run out (tad_debug_lost_waits; norm.cu)
+namespace tadr { extern std::atomic<int> lost_waits; }
 
 namespace tadr {
 
