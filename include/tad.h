@@ -287,7 +287,8 @@ tad_status tad_debug_status(const tad_plan *plan, void *workspace, void *cuda_st
  *   - Workspaces: device memory of at least the bytes that the matching function says, 256-byte aligned, owned by the
  *     caller; its content need not be kept between calls, and calls that share one must not overlap on the device.
  *   - Limits: 0 <= n_rows, n_tokens < 2^31, 0 <= width < 2^24; offsets are computed in 64 bits.  Sizes of zero are
- *     allowed; TAD_ERR_UNSUPPORTED beyond.  NULL descriptors or data that a call needs, a stride below the width, an unknown
+ *     allowed; TAD_ERR_UNSUPPORTED beyond, and where both together ask for more blocks than a launch has (2^31; matrices of
+ *     terabytes).  NULL descriptors or data that a call needs, a stride below the width, an unknown
  *     type, a misaligned packed matrix: TAD_ERR_INVALID_ARG.
  */
 typedef enum { TAD_F32 = 0, TAD_BF16 = 1, TAD_F16 = 2 } tad_type;

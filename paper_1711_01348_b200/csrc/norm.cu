@@ -11,7 +11,7 @@
 // variance is the mean of the squared deviations of the registers (no difference of large sums).  Weights stay in registers
 // over all rows.  The backward pass keeps its share of dw and db there too and writes them once a block, as a plane of partial
 // sums; a second kernel adds the planes up in a fixed order.  Rows longer than a cluster holds are read twice or three times.
-// Measured, 8192 x 4096: fp32 forward 43 us, backward 67 (6.2, 6.0 TB/s); bf16 26.5, 40 (5.1, 5.0 TB/s: of the backward pass the rows take 32, which
+// Measured, 8192 x 4096: fp32 forward 43 us, backward 67 (6.2, 6.0 TB/s); bf16 26, 40 (5.2, 5.0 TB/s: of the backward pass the rows take 32, which
 // is the memory's rate, its start 2, the join of the partial sums in a block and of the blocks 1 and 2.7).
 #include <cooperative_groups.h>
 
@@ -1044,7 +1044,8 @@ template <class T>
 cudaError_t forward(const Params &P, const Shape &s, bool eights, bool keep, cudaStream_t stream)
 {
     if (P.width > HELD) return tad_launch(tad_norm_forward_long_kernel<T>, (unsigned)std::min<int64_t>(P.n_rows, 2 * SMS), LARGE, 0, stream, P);
-    // Rows that a cluster would hold, by one block.  (Of few rows a cluster each is faster: 16 x 16384 4.5 us for 6.6, 200 x 8192 5.4 for 6.4, 300 x 8192
+    // Rows that a cluster would hold, by one block, as far as two rows and the weights fit into 220 KB: 13312 columns of fp32, 18432 of 16-bit types
+    // (2048 x 16384 bf16 35 us, 2048 x 18440 by clusters 116).  (Of few rows a cluster each is faster: 16 x 16384 4.5 us for 6.6, 200 x 8192 5.4 for 6.4, 300 x 8192
     // 6.9 for 6.7, 1000 x 8192 14 for 10.  Rows up to 4096 in this form: 8192 x 4096 25.3 for 26.5, but 8192 x 2560 22.4 for 20.2, 20000 x 1024 25.6
     // for 17.6, 1000 x 2048 5.6 for 4.5.)
     if (eights && !keep && s.by == BY_CLUSTER && P.width <= WIDE_BLOCK * WIDE_E<T> && P.n_rows >= 2 * SMS) {
@@ -1158,7 +1159,7 @@ tad_status tad_layernorm_forward(const tad_rows *x, int64_t n_rows, int64_t widt
     const Shape s = shape_of(width, FORWARD_BLOCK, FORWARD_E);
     P.group = s.group;
     const bool eights = width % 8 == 0 && by_eights(x) && by_eights(y);
-    // The checkpoint of fp32 rows in the norm's own pass (8192 x 4096: 53 us for 71); of 16-bit rows, where the pass has no instructions to
+    // The checkpoint of fp32 rows in the norm's own pass (8192 x 4096: 51 us for 71); of 16-bit rows, where the pass has no instructions to
     // spare, by the packing kernel, which leaves x in L2 for the next one (16384 x 2048 bf16 43 us either way, 8192 x 4096 44 us for 46).
     const bool keep = checkpoint && x->type == TAD_F32 && eights && width <= HELD;
     if (keep) { P.kq = checkpoint->q; P.kqs = checkpoint->q_stride; P.kscale = checkpoint->scale; P.kss = checkpoint->scale_stride; }

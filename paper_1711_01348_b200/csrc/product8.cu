@@ -11,8 +11,8 @@
 // bring the scales of 512 elements at a time from memory into tensor memory, a warp issues the MMAs and eight warps empty the
 // accumulator.  Large products run on pairs of blocks (PAIR, clusters of two SMs): a tile of 256 x 256, each block holds 128 rows of p and
 // of q and half of the accumulator, and the first block issues the MMAs of both.  What bounds those is L2: at the full rate of the
-// tensor cores single tiles of 128 x 256 would read 27 TB/s from it.  Measured, bf16 out: 8192 x 4096 x 4096 99 us (2.8 PFLOP/s; 112 us
-// in a row without a pause, where the power limit sets the clock), 8192 x 8192 x 8192 361 us (3.0); with one MMA of four left the
+// tensor cores single tiles of 128 x 256 would read 27 TB/s from it.  Measured, bf16 out: 8192 x 4096 x 4096 99 us (2.8 PFLOP/s; 112 - 120 us
+// in a row without a pause, where the power limit sets the clock), 8192 x 8192 x 8192 361 - 374 us (3.0 - 2.9); with one MMA of four left the
 // loop takes 64 of the 99 us, so the tensor cores and their clock are what remains.
 #include <cuda.h>
 
@@ -436,7 +436,7 @@ tad_product8_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_cons
 // ---- few rows ----
 
 // Up to four rows on one side and little work: bound by its launch and one round of loads.  A warp takes two rows of the other operand and
-// sixteen elements of k a lane and step, the few rows come from the first-level cache.  Four instructions an element and row make it
+// sixteen elements of k a lane and step, the few rows come from the first-level cache.  Five instructions an element, of one row, make it
 // slower than the tensor cores from some 20 million multiply-adds on; us, these / those: 1 x 256 x 256 2.0 / 4.4, 4 x 1000 x 1000 4.3 / 5.8,
 // 1 x 4096 x 4096 6.3 / 7.5, 2 x 4096 x 4096 8.9 / 7.5, 1 x 65536 x 512 15 / 11, 1 x 16384 x 8192 35 / 27.
 constexpr int FEW = 4, FEW_ROWS = 2;
